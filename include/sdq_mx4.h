@@ -1,0 +1,78 @@
+/*
+ * sdq_mx4.h -- C-ABI of the microscaled 4-bit operators: quantization and product of plain (not decomposed) matrices, and the
+ * mixture-of-experts layer of a few tokens over experts in that format.  Conventions, status codes and ownership as in sdq.h.
+ *
+ * Formats.  An element is an E2M1 code (0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign).
+ *   SDQ_FMT_MXFP4  one E8M0 scale 2^(c - 127) per 32 elements of a row; scale_rule as for the decomposition's Q-Vectors
+ *                  (SDQ_SCALE_OCP_FLOOR, SDQ_SCALE_CEIL_NOSAT).
+ *   SDQ_FMT_NVFP4  one unsigned E4M3 scale per 16 elements under one fp32 factor per row.  sdq_mx4_quantize chooses the factor
+ *                  2^t, t the smallest integer >= -126 with the row's largest magnitude <= 2688 * 2^t (0 for a row of zeros), and as
+ *                  scale the E4M3 value nearest to a / (6 * 2^t) (ties to even, at least 2^-9 unless a = 0); scale_rule is
+ *                  ignored.  sdq_mx4_import takes any factors (a per-tensor factor is the same one for every row).
+ * Elements are the E2M1 values nearest to x / (scale * factor), ties to even, saturating; both formats decide as the exact
+ * quotient does.  Infinities count as the largest finite number of their type.  A block that holds a NaN gets the NaN scale code,
+ * and every product with it is NaN.
+ *
+ * Sizes.  Any R, K >= 1 (rows that end inside a block are quantized over the elements they have).  Rows may be strided;
+ * pointers are aligned to their element, buffers to 256 bytes.  Every call asks for the device that is current.
+ */
+#ifndef SDQ_MX4_H_
+#define SDQ_MX4_H_
+
+#include "sdq.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+enum { SDQ_FMT_MXFP4 = 0, SDQ_FMT_NVFP4 = 1 };
+enum { SDQ_BF16 = 0, SDQ_FP16 = 1, SDQ_FP32 = 2 };            /* element types of unquantized operands */
+
+/* Host-side descriptor of a quantized matrix, or of the stacked matrices of E experts (plain data, may be copied; `dev`
+ * stays owned by the caller).  off: 0 records (linear) / codes (experts)  1 scales (experts)  2 row factors (NVFP4) */
+typedef struct {
+  void* dev;
+  size_t bytes;
+  int64_t E, R, K;      /* E = 0: a linear matrix [R, K]; else E matrices [R, K] in the experts' layout */
+  int32_t fmt;
+  int32_t reserved;
+  size_t off[3];
+} sdq_mx4_t;
+
+/* Bytes of the buffer of an R x K matrix. */
+sdq_status_t sdq_mx4_size(int64_t R, int64_t K, int32_t fmt, size_t* bytes);
+
+/* X (device) [R][ldx] of `dtype` -> codes and scales in `buf`, in the tiled layout sdq_mx4_linear streams (a weight matrix and a
+ * batch of activations are stored alike).  One launch.  Asynchronous on `stream`. */
+sdq_status_t sdq_mx4_quantize(const void* X, int32_t dtype, int64_t R, int64_t K, int64_t ldx, int32_t fmt, int32_t scale_rule,
+                              void* buf, size_t bytes, sdq_mx4_t* out, void* stream);
+
+/* Codes and scales as checkpoints hold them -> the tiled layout.  codes (device) [R][ceil(K/2)], two to a byte, the lower k in the
+ * low nibble; scales (device) [R][ceil(K/32)] E8M0 or [R][ceil(K/16)] E4M3; factor (device) [R] fp32, NVFP4 only, NULL = 1. */
+sdq_status_t sdq_mx4_import(const uint8_t* codes, const uint8_t* scales, const float* factor, int64_t R, int64_t K, int32_t fmt,
+                            void* buf, size_t bytes, sdq_mx4_t* out, void* stream);
+
+/* The reverse: plain arrays of the same shapes (factor may be NULL).  Also for experts: rows e * R + r. */
+sdq_status_t sdq_mx4_export(const sdq_mx4_t* q, uint8_t* codes, uint8_t* scales, float* factor, void* stream);
+
+/* The values that are held, rounded to `dtype` (bf16 and fp32 hold them exactly unless they leave their range):
+ * out (device) [R][ldo], for experts [E * R][ldo]. */
+sdq_status_t sdq_mx4_dequantize(const sdq_mx4_t* q, void* out, int32_t dtype, int64_t ldo, void* stream);
+
+/* Y [M][ldy] (dtype) = Xq Wq^T + bias, Xq [M, K] and Wq [N, K] of one format, products and sums in fp32 on the tensor core, bias
+ * (device) [N] of `dtype` or NULL; rounded once.  Errors: SHAPE where K differs, UNSUPPORTED where the formats do or an
+ * operand has the experts' layout.  A wait that gives up sets the flag that sdq_device_status reports. */
+sdq_status_t sdq_mx4_linear(const sdq_mx4_t* Xq, const sdq_mx4_t* Wq, const void* bias, int32_t dtype, void* Y, int64_t ldy, void* stream);
+
+/* The experts' form: E stacked matrices [E][R][K] in MXFP4. */
+sdq_status_t sdq_mx4_experts_size(int64_t E, int64_t R, int64_t K, size_t* bytes);
+/* W (device) [E][R][K] contiguous, of `dtype` */
+sdq_status_t sdq_mx4_experts_quantize(const void* W, int32_t dtype, int64_t E, int64_t R, int64_t K, int32_t scale_rule,
+                                      void* buf, size_t bytes, sdq_mx4_t* out, void* stream);
+sdq_status_t sdq_mx4_experts_import(const uint8_t* codes, const uint8_t* scales, int64_t E, int64_t R, int64_t K,
+                                    void* buf, size_t bytes, sdq_mx4_t* out, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif

@@ -31,6 +31,7 @@ def gran_keep(n: int) -> int:
 SCALE_OCP_FLOOR, SCALE_CEIL_NOSAT, SCALE_UE4M3 = 0, 1, 2
 ORDER_LARGE, ORDER_SMALL = 0, 1
 OUT_E4M3, OUT_INT8 = 0, 1
+FMT_MXFP4, FMT_NVFP4 = 0, 1                 # plain microscaled formats: E8M0 scale per 32, E4M3 scale per 16 under a row factor
 
 STATUS = ["ok", "invalid_arg", "shape", "alignment", "unsupported", "buffer_too_small", "nonfinite", "cuda", "timeout"]
 
@@ -68,9 +69,15 @@ class _ActCanon(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("xq4_code", "xq4_scale", "xq8_code", "xq8_sexp")]
 
 
+class _Mx4(ctypes.Structure):
+    _fields_ = [("dev", ctypes.c_void_p), ("bytes", ctypes.c_size_t), ("E", ctypes.c_int64), ("R", ctypes.c_int64), ("K", ctypes.c_int64),
+                ("fmt", ctypes.c_int32), ("reserved", ctypes.c_int32), ("off", ctypes.c_size_t * 3)]
+
+
 EXPORTS = ["sdq_packed_size", "sdq_decompose", "sdq_decompose_metric", "sdq_channel_norm", "sdq_packed_export", "sdq_packed_attach", "sdq_packed_compact_size", "sdq_packed_compact", "sdq_act_size", "sdq_quantize_act", "sdq_act_export",
            "sdq_linear", "sdq_linear_f32", "sdq_workspace_size", "sdq_workspace_init", "sdq_linear_ws", "sdq_linear_f32_ws", "sdq_linear_noalloc",
-           "sdq_linear_group", "sdq_linear_group_f32", "sdq_linear_group_x", "sdq_linear_group_x_f32", "sdq_linear_group_x_ws", "sdq_linear_group_x_f32_ws", "sdq_diag_l2_copy", "sdq_diag_wait_timeout", "sdq_diag_decompose_timeout", "sdq_diag_linear_plan", "sdq_diag_linear_rings", "sdq_diag_group_plan", "sdq_device_status", "sdq_status_string"]
+           "sdq_linear_group", "sdq_linear_group_f32", "sdq_linear_group_x", "sdq_linear_group_x_f32", "sdq_linear_group_x_ws", "sdq_linear_group_x_f32_ws", "sdq_mx4_size", "sdq_mx4_quantize", "sdq_mx4_import", "sdq_mx4_export", "sdq_mx4_dequantize", "sdq_mx4_linear",
+           "sdq_mx4_experts_size", "sdq_mx4_experts_quantize", "sdq_mx4_experts_import", "sdq_diag_l2_copy", "sdq_diag_wait_timeout", "sdq_diag_decompose_timeout", "sdq_diag_linear_plan", "sdq_diag_linear_rings", "sdq_diag_group_plan", "sdq_device_status", "sdq_status_string"]
 
 _lib = None
 
@@ -105,6 +112,16 @@ def lib() -> ctypes.CDLL:
         L.sdq_linear_noalloc.argtypes = [ctypes.POINTER(_Act), ctypes.POINTER(_Packed), vp, i64, vp]
         L.sdq_linear_group.argtypes = [ctypes.c_int, vp, vp, vp, vp, vp]
         L.sdq_linear_group_f32.argtypes = [ctypes.c_int, vp, vp, vp, vp, vp]
+        i32, m4 = ctypes.c_int32, ctypes.POINTER(_Mx4)
+        L.sdq_mx4_size.argtypes = [i64, i64, i32, ctypes.POINTER(sz)]
+        L.sdq_mx4_quantize.argtypes = [vp, i32, i64, i64, i64, i32, i32, vp, sz, m4, vp]
+        L.sdq_mx4_import.argtypes = [vp, vp, vp, i64, i64, i32, vp, sz, m4, vp]
+        L.sdq_mx4_export.argtypes = [m4, vp, vp, vp, vp]
+        L.sdq_mx4_dequantize.argtypes = [m4, vp, i32, i64, vp]
+        L.sdq_mx4_linear.argtypes = [m4, m4, vp, i32, vp, i64, vp]
+        L.sdq_mx4_experts_size.argtypes = [i64, i64, i64, ctypes.POINTER(sz)]
+        L.sdq_mx4_experts_quantize.argtypes = [vp, i32, i64, i64, i64, i32, vp, sz, m4, vp]
+        L.sdq_mx4_experts_import.argtypes = [vp, vp, i64, i64, i64, vp, sz, m4, vp]
         L.sdq_device_status.argtypes = [vp]
         L.sdq_status_string.argtypes = [ctypes.c_int]
         L.sdq_status_string.restype = ctypes.c_char_p
@@ -411,6 +428,190 @@ def act_export(xq: QuantAct) -> dict:
     c = _ActCanon(*[t[n].data_ptr() for n in ("xq4_code", "xq4_scale", "xq8_code", "xq8_sexp")])
     _check(lib().sdq_act_export(ctypes.byref(xq.desc), ctypes.byref(c), _stream()), "sdq_act_export")
     return t
+
+
+# ---- plain microscaled 4-bit matrices and the expert layer over them (include/sdq_mx4.h) ------------------------------------
+_DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+
+
+@dataclass
+class Mx4Matrix:
+    """A matrix in MXFP4 or NVFP4 (weights or activations): device buffer plus host descriptor."""
+    buf: torch.Tensor
+    desc: _Mx4
+    R: int
+    K: int
+    fmt: int
+
+
+@dataclass
+class Mx4Experts:
+    """E stacked weight matrices [R, K] in MXFP4, in the form sdq_mx4_moe streams."""
+    buf: torch.Tensor
+    desc: _Mx4
+    E: int
+    R: int
+    K: int
+
+
+def _operand(t, name: str, dtypes, dim: int, rows_only: bool = True) -> torch.Tensor:
+    """a CUDA tensor of the current device, of one of the types and as many dimensions, its last one dense"""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("%s must be a tensor" % name)
+    _need_cuda(t, name)
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError("%s is on %s, the current device is cuda:%d" % (name, t.device, torch.cuda.current_device()))
+    if t.dtype not in dtypes:
+        raise ValueError("%s has type %s, not one of %s" % (name, t.dtype, ", ".join(str(d) for d in dtypes)))
+    if t.dim() != dim:
+        raise ValueError("%s has %d dimensions, not %d" % (name, t.dim(), dim))
+    if t.shape[-1] > 1 and t.stride(-1) != 1 or not rows_only and not t.is_contiguous():
+        raise ValueError("%s must be contiguous%s" % (name, " along its last dimension" if rows_only else ""))
+    return t
+
+
+def _row_stride(t: torch.Tensor) -> int:
+    """elements from one row to the next (of a single row: its length)"""
+    if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+        raise ValueError("rows overlap")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _buffer(buf, nbytes: int, device) -> torch.Tensor:
+    if buf is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    return _operand(buf, "buf", (torch.uint8,), 1, False)
+
+
+def _same_device(q, name: str):
+    if q.buf.device.index != torch.cuda.current_device():
+        raise ValueError("%s is on %s, the current device is cuda:%d" % (name, q.buf.device, torch.cuda.current_device()))
+
+
+def mx4_size(R: int, K: int, fmt: int = FMT_MXFP4) -> int:
+    b = ctypes.c_size_t()
+    _check(lib().sdq_mx4_size(R, K, fmt, ctypes.byref(b)), "sdq_mx4_size")
+    return b.value
+
+
+def sdq_mx4_quantize(X: torch.Tensor, fmt: int = FMT_MXFP4, rule: int = SCALE_OCP_FLOOR, buf: torch.Tensor | None = None) -> Mx4Matrix:
+    """X [R, K] (bf16, fp16 or fp32 CUDA tensor; any sizes, rows may be strided) -> MXFP4 or NVFP4, weights and activations alike."""
+    _operand(X, "X", _DTYPES, 2)
+    R, K = X.shape
+    buf = _buffer(buf, mx4_size(R, K, fmt), X.device)
+    d = _Mx4()
+    _check(lib().sdq_mx4_quantize(X.data_ptr(), _DTYPES[X.dtype], R, K, _row_stride(X), fmt, rule, buf.data_ptr(), buf.numel(), ctypes.byref(d), _stream()),
+           "sdq_mx4_quantize")
+    return Mx4Matrix(buf, d, R, K, fmt)
+
+
+def sdq_mx4_import(codes: torch.Tensor, scales: torch.Tensor, fmt: int = FMT_MXFP4, K: int | None = None, factor: torch.Tensor | None = None,
+                   buf: torch.Tensor | None = None) -> Mx4Matrix:
+    """Packed codes [R, ceil(K / 2)] and scale codes [R, ceil(K / 32)] (NVFP4: ceil(K / 16), with an fp32 factor [R] or None) as a
+    checkpoint holds them -> Mx4Matrix.  K defaults to twice the code bytes."""
+    _operand(codes, "codes", (torch.uint8,), 2, False)
+    R = codes.shape[0]
+    K = 2 * codes.shape[1] if K is None else K
+    nbytes = mx4_size(R, K, fmt)
+    _operand(scales, "scales", (torch.uint8,), 2, False)
+    if codes.shape[1] != (K + 1) // 2 or tuple(scales.shape) != (R, -(-K // (16 if fmt == FMT_NVFP4 else 32))):
+        raise ValueError("codes %s and scales %s do not belong to a [%d, %d] matrix" % (tuple(codes.shape), tuple(scales.shape), R, K))
+    if factor is not None:
+        if fmt != FMT_NVFP4:
+            raise ValueError("only NVFP4 has row factors")
+        _operand(factor, "factor", (torch.float32,), 1, False)
+        if factor.shape[0] != R:
+            raise ValueError("factor has %d entries for %d rows" % (factor.shape[0], R))
+    buf = _buffer(buf, nbytes, codes.device)
+    d = _Mx4()
+    _check(lib().sdq_mx4_import(codes.data_ptr(), scales.data_ptr(), None if factor is None else factor.data_ptr(), R, K, fmt, buf.data_ptr(), buf.numel(),
+                                ctypes.byref(d), _stream()), "sdq_mx4_import")
+    return Mx4Matrix(buf, d, R, K, fmt)
+
+
+def mx4_export(q) -> dict:
+    """Plain arrays of an Mx4Matrix or Mx4Experts: code (two to a byte), scale and, for NVFP4, factor, shaped as sdq_mx4_import and
+    sdq_mx4_experts_import take them."""
+    _same_device(q, "q")
+    experts, nv = isinstance(q, Mx4Experts), q.desc.fmt == FMT_NVFP4
+    lead = (q.E, q.R) if experts else (q.R,)
+    t = dict(code=torch.empty(lead + ((q.K + 1) // 2,), dtype=torch.uint8, device=q.buf.device),
+             scale=torch.empty(lead + (-(-q.K // (16 if nv else 32)),), dtype=torch.uint8, device=q.buf.device))
+    if nv:
+        t["factor"] = torch.empty(q.R, dtype=torch.float32, device=q.buf.device)
+    _check(lib().sdq_mx4_export(ctypes.byref(q.desc), t["code"].data_ptr(), t["scale"].data_ptr(), t["factor"].data_ptr() if nv else None, _stream()),
+           "sdq_mx4_export")
+    return t
+
+
+def sdq_mx4_dequantize(q, dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None) -> torch.Tensor:
+    """The values an Mx4Matrix ([R, K]) or Mx4Experts ([E, R, K]) holds."""
+    _same_device(q, "q")
+    if dtype not in _DTYPES:
+        raise ValueError("no output of type %s" % dtype)
+    experts = isinstance(q, Mx4Experts)
+    shape = (q.E, q.R, q.K) if experts else (q.R, q.K)
+    if out is None:
+        out = torch.empty(shape, dtype=dtype, device=q.buf.device)
+    else:
+        _operand(out, "out", (dtype,), len(shape), not experts)
+        if tuple(out.shape) != shape:
+            raise ValueError("out has shape %s, not %s" % (tuple(out.shape), shape))
+    _check(lib().sdq_mx4_dequantize(ctypes.byref(q.desc), out.data_ptr(), _DTYPES[dtype], q.K if experts else _row_stride(out), _stream()), "sdq_mx4_dequantize")
+    return out
+
+
+def sdq_mx4_experts(W: torch.Tensor, rule: int = SCALE_OCP_FLOOR) -> Mx4Experts:
+    """W [E, R, K] (bf16, fp16 or fp32, contiguous CUDA tensor) -> the experts' MXFP4 form."""
+    _operand(W, "W", _DTYPES, 3, False)
+    E, R, K = W.shape
+    b = ctypes.c_size_t()
+    _check(lib().sdq_mx4_experts_size(E, R, K, ctypes.byref(b)), "sdq_mx4_experts_size")
+    buf = torch.empty(b.value, dtype=torch.uint8, device=W.device)
+    d = _Mx4()
+    _check(lib().sdq_mx4_experts_quantize(W.data_ptr(), _DTYPES[W.dtype], E, R, K, rule, buf.data_ptr(), buf.numel(), ctypes.byref(d), _stream()),
+           "sdq_mx4_experts_quantize")
+    return Mx4Experts(buf, d, E, R, K)
+
+
+def sdq_mx4_experts_import(codes: torch.Tensor, scales: torch.Tensor, K: int | None = None) -> Mx4Experts:
+    """Packed codes [E, R, ceil(K / 2)] and E8M0 scale codes [E, R, ceil(K / 32)] as a checkpoint holds them -> the experts' form."""
+    _operand(codes, "codes", (torch.uint8,), 3, False)
+    _operand(scales, "scales", (torch.uint8,), 3, False)
+    E, R = codes.shape[:2]
+    K = 2 * codes.shape[2] if K is None else K
+    b = ctypes.c_size_t()
+    _check(lib().sdq_mx4_experts_size(E, R, K, ctypes.byref(b)), "sdq_mx4_experts_size")
+    if codes.shape[2] != (K + 1) // 2 or tuple(scales.shape) != (E, R, -(-K // 32)):
+        raise ValueError("codes %s and scales %s do not belong to [%d, %d, %d] experts" % (tuple(codes.shape), tuple(scales.shape), E, R, K))
+    buf = torch.empty(b.value, dtype=torch.uint8, device=codes.device)
+    d = _Mx4()
+    _check(lib().sdq_mx4_experts_import(codes.data_ptr(), scales.data_ptr(), E, R, K, buf.data_ptr(), buf.numel(), ctypes.byref(d), _stream()),
+           "sdq_mx4_experts_import")
+    return Mx4Experts(buf, d, E, R, K)
+
+
+def sdq_mx4_linear(xq: Mx4Matrix, wq: Mx4Matrix, bias: torch.Tensor | None = None, out: torch.Tensor | None = None,
+                   dtype: torch.dtype | None = None) -> torch.Tensor:
+    """Y [M, N] = Xq Wq^T + bias, fp32 sums on the tensor core, rounded once to `dtype` (of `out` if that is given, else bf16)."""
+    _same_device(xq, "xq")
+    _same_device(wq, "wq")
+    dtype = dtype or (out.dtype if out is not None else torch.bfloat16)
+    if dtype not in _DTYPES:
+        raise ValueError("no output of type %s" % dtype)
+    if bias is not None:
+        _operand(bias, "bias", (dtype,), 1, False)
+        if bias.shape[0] != wq.R:
+            raise ValueError("bias has %d entries for %d outputs" % (bias.shape[0], wq.R))
+    if out is None:
+        out = torch.empty((xq.R, wq.R), dtype=dtype, device=wq.buf.device)
+    else:
+        _operand(out, "out", (dtype,), 2)
+        if tuple(out.shape) != (xq.R, wq.R):
+            raise ValueError("out has shape %s, not %s" % (tuple(out.shape), (xq.R, wq.R)))
+    _check(lib().sdq_mx4_linear(ctypes.byref(xq.desc), ctypes.byref(wq.desc), None if bias is None else bias.data_ptr(), _DTYPES[dtype], out.data_ptr(),
+                                _row_stride(out), _stream()), "sdq_mx4_linear")
+    return out
 
 
 def device_status() -> int:

@@ -15,10 +15,12 @@ LIB = os.path.join(_HERE, "libsdq_b200.so")
 # C++ against torch's headers: the versions it was built for are part of the name, so a module of another torch is never loaded
 BINDING = os.path.join(_HERE, "_binding-%s-torch%s.so" % (sys.implementation.cache_tag, torch.__version__))
 BINDING_SOURCE = "sdq_python.cpp"
-SOURCES = ["sdq_api.cu", "sdq_pack.cu", "sdq_quant_act.cu", "sdq_linear.cu", "sdq_linear_pair.cu", "sdq_linear_group.cu", "sdq_plain.cu", "sdq_calib.cu", "sdq_diag.cu"]
-HEADERS = ["sdq_internal.h", "sdq_layout.h", "sdq_linear.h", "sdq_plain.h", "sdq_ptx.cuh", "sdq_codec.cuh", os.path.join("..", "..", "include", "sdq.h"), os.path.join("..", "..", "include", "sdq_diag.h")]
+SOURCES = ["sdq_api.cu", "sdq_pack.cu", "sdq_quant_act.cu", "sdq_linear.cu", "sdq_linear_pair.cu", "sdq_linear_group.cu", "sdq_plain.cu", "sdq_calib.cu", "sdq_diag.cu",
+           "mx4/quant.cu", "mx4/linear.cu"]
+HEADERS = ["sdq_internal.h", "sdq_layout.h", "sdq_linear.h", "sdq_plain.h", "sdq_ptx.cuh", "sdq_codec.cuh", os.path.join("..", "..", "include", "sdq.h"), os.path.join("..", "..", "include", "sdq_diag.h"),
+           os.path.join("mx4", "layout.h"), os.path.join("..", "..", "include", "sdq_mx4.h")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-shared",
-              "-Xcompiler", "-fPIC"]
+              "-Xcompiler", "-fPIC", "--threads", "0"]
 
 
 def _stale() -> bool:

@@ -1,0 +1,526 @@
+// Product of two microscaled 4-bit matrices  Y = Xq Wq^T + bias  on the block-scaled tensor-core kinds
+// (kind::mxf4 .block32 for MXFP4, kind::mxf4nvf4 .block16 for NVFP4; fp32 accumulators in tensor memory).
+//
+// Few tokens (mx4_linear_narrow_kernel): weights stream through, so their rows are the MMA's 128 rows and the tokens its columns.
+// The CTAs of a cluster split K of one row tile, keep their fp32 partial tiles in shared memory and sum them there in a fixed
+// order: no scratch in global memory, no atomics, the same result every time.
+//
+// Many tokens (mx4_linear_wide_kernel): CTA pairs, 256 tokens x 256 weight rows a task, K in records of 256.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <type_traits>
+
+#include "../sdq_internal.h"
+#include "layout.h"
+#include "../sdq_ptx.cuh"
+
+namespace sdq {
+namespace mx4 {
+
+struct GemmParams {
+  const uint8_t *x, *w;            // records of the activations and of the weights
+  const float *fx, *fw;            // row factors (NVFP4)
+  const void* bias;
+  void* Y;
+  uint32_t* flags;
+  int64_t M, N, ldy;
+  int32_t kb;                      // records along K
+  int32_t m_tiles, n_tiles;        // row tiles of 128 of both
+  int32_t T;                       // narrow: token columns of a tile
+  int32_t nslot;
+  int32_t pt_m, pt_n, tasks;       // wide: tiles of 256, tasks
+};
+
+template <int DT> struct Out;
+template <> struct Out<SDQ_BF16> { using type = __nv_bfloat16; };
+template <> struct Out<SDQ_FP16> { using type = __half; };
+template <> struct Out<SDQ_FP32> { using type = float; };
+template <int DT> __device__ __forceinline__ typename Out<DT>::type to_out(float v) {
+  if constexpr (DT == SDQ_BF16) return __float2bfloat16_rn(v);
+  else if constexpr (DT == SDQ_FP16) return __float2half_rn(v);
+  else return v;
+}
+template <int DT> __device__ __forceinline__ float from_out(typename Out<DT>::type v) {
+  if constexpr (DT == SDQ_BF16) return __bfloat162float(v);
+  else if constexpr (DT == SDQ_FP16) return __half2float(v);
+  else return v;
+}
+
+// ---- few tokens -----------------------------------------------------------------------------------------------------------
+constexpr int NARROW_THREADS = 192;                  // producer, MMA issuer, four epilogue warps
+constexpr uint32_t NARROW_TAIL = 256 + 128;          // barriers, and room to align the ring to 128 bytes
+constexpr int NARROW_MAX_SLOTS = 12;
+// slot = | weight record | codes of T tokens | scale atoms of the tokens |
+__host__ __device__ constexpr uint32_t narrow_slot(int fmt, int T) { return record(fmt) + (uint32_t)T * 128u + atoms(fmt) * ATOM; }
+
+// sum over the cluster's CTAs, in their order, of the float at `saddr`
+__device__ __forceinline__ float sum_over_cluster(uint32_t saddr, uint32_t ctas) {
+  float s = 0.0f;
+  for (uint32_t c = 0; c < ctas; ++c) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(ptx::mapa_u32(saddr, c)) : "memory");
+    s += v;
+  }
+  return s;
+}
+
+template <int FMT, int DT>
+__global__ void __launch_bounds__(NARROW_THREADS)
+mx4_linear_narrow_kernel(const __grid_constant__ GemmParams p)
+{
+  using T_out = typename Out<DT>::type;
+  constexpr uint32_t NA = atoms(FMT), REC = record(FMT), SET = 8u * NA;       // TMEM columns of one set of scales: 4 NA weights, 4 NA tokens
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* sm = smem_raw + ((128 - (ptx::smem_u32(smem_raw) & 127)) & 127);
+  const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t T = (uint32_t)p.T, SLOT = narrow_slot(FMT, p.T), NSLOT = (uint32_t)p.nslot;
+  uint64_t* full = reinterpret_cast<uint64_t*>(sm + (size_t)NSLOT * SLOT);
+  uint64_t* empty = full + NARROW_MAX_SLOTS;
+  uint64_t* acc_full = empty + NARROW_MAX_SLOTS;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_full + 1);
+  static_assert((2 * NARROW_MAX_SLOTS + 1) * 8 + 4 <= 256);
+  uint32_t ks;
+  asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(ks));
+  const uint32_t rank = ptx::cluster_ctarank();
+  const int nt = (int)(blockIdx.x / ks), mt = (int)blockIdx.y;
+  const int k0 = (int)(rank * (uint32_t)p.kb / ks), n_rec = (int)((rank + 1) * (uint32_t)p.kb / ks) - k0;
+  const uint8_t* w = p.w + ((size_t)nt * p.kb + k0) * REC;
+  const uint8_t* x = p.x + ((size_t)mt * p.kb + k0) * REC;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      ptx::griddep_launch_dependents();
+      for (uint32_t i = 0; i < NSLOT; ++i) { ptx::mbar_init(&full[i], 1); ptx::mbar_init(&empty[i], 1); }
+      ptx::mbar_init(acc_full, 1);
+      ptx::fence_barrier_init();
+      // the weights may be what the kernel in front writes: they are brought into L2, which holds what is written, not into
+      // shared memory
+      for (int i = 0; i < min(n_rec, (int)NSLOT); ++i) ptx::bulk_prefetch_l2(w + (size_t)i * REC, REC);
+    }
+  } else if (warp == 1) {
+    ptx::tmem_alloc(tmem_slot, 256);
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  const uint32_t tmem = *tmem_slot, sets = tmem + (T <= 128 ? 128u : T);
+  ptx::griddep_wait();
+
+  bool ok = true;
+  if (warp == 0) {
+    if (lane == 0) {
+      for (int i = 0; i < n_rec && ok; ++i) {
+        const uint32_t s = (uint32_t)i % NSLOT;
+        if (i >= (int)NSLOT && !(ok = ptx::mbar_wait(&empty[s], (((uint32_t)i / NSLOT) & 1u) ^ 1u))) break;
+        uint8_t* st = sm + (size_t)s * SLOT;
+        ptx::mbar_expect_tx(&full[s], SLOT);
+        ptx::bulk_g2s(st, w + (size_t)i * REC, REC, &full[s]);
+        ptx::bulk_g2s(st + REC, x + (size_t)i * REC, T * 128u, &full[s]);
+        ptx::bulk_g2s(st + REC + T * 128u, x + (size_t)i * REC + CODES, NA * ATOM, &full[s]);
+      }
+      if (!ok) atomicOr(&p.flags[FLAG_TIMEOUT], 1u);
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    if (lane == 0) {
+      // copies to tensor memory and MMAs of one thread execute in issue order: two alternating sets of scales serve all slots
+      const uint32_t id0 = ptx::idesc_block_scaled(128, T, 1, false, 0, 0) ^ (FMT == SDQ_FMT_NVFP4 ? 1u << 23 : 0u);
+      const uint32_t id2 = ptx::idesc_block_scaled(128, T, 1, false, 2, 2);
+      for (int i = 0; i < n_rec && ok; ++i) {
+        const uint32_t s = (uint32_t)i % NSLOT;
+        if (!(ok = ptx::mbar_wait(&full[s], ((uint32_t)i / NSLOT) & 1u))) break;
+        ptx::tc_fence_after();
+        const uint32_t st = ptx::smem_u32(sm) + s * SLOT, sfa = sets + (i & 1) * SET, sfb = sfa + 4 * NA;
+        const uint64_t da = ptx::smem_desc(st, 128, 1024), db = ptx::smem_desc(st + REC, 128, 1024);
+        const uint64_t ca = ptx::smem_desc(st + CODES, 0, 128), cb = ptx::smem_desc(st + REC + T * 128u, 0, 128);
+#pragma unroll
+        for (uint32_t a = 0; a < NA; ++a) {
+          ptx::tc_cp_32x128b_warpx4(sfa + 4 * a, ca + a * (ATOM >> 4));
+          ptx::tc_cp_32x128b_warpx4(sfb + 4 * a, cb + a * (ATOM >> 4));
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) {                       // 64 K each: two adjacent core matrices
+          const uint32_t acc = i || j ? 1u : 0u;
+          if constexpr (FMT == SDQ_FMT_NVFP4) ptx::mma_nvf4(tmem, da + ((256 * j) >> 4), db + ((256 * j) >> 4), id0, sfa + 4 * j, sfb + 4 * j, acc);
+          else ptx::mma_mxf4(tmem, da + ((256 * j) >> 4), db + ((256 * j) >> 4), j & 1 ? id2 : id0, sfa + 4 * (j >> 1), sfb + 4 * (j >> 1), acc);
+        }
+        ptx::tc_commit(&empty[s]);
+      }
+      if (ok) ptx::tc_commit(acc_full);
+      else atomicOr(&p.flags[FLAG_TIMEOUT], 1u);
+    }
+    __syncwarp();
+  } else {
+    // warp w owns TMEM lanes 32 (w % 4) ..: weight rows
+    const uint32_t q = warp & 3, row = q * 32 + lane;
+    const int64_t n = (int64_t)nt * ROWS + row, m0 = (int64_t)mt * 128;
+    const int valid = (int)min((int64_t)T, p.M - m0);
+    float fw = 1.0f, b = 0.0f;
+    if (n < p.N) {
+      if (FMT == SDQ_FMT_NVFP4) fw = p.fw[n];
+      if (p.bias) b = from_out<DT>(reinterpret_cast<const T_out*>(p.bias)[n]);
+    }
+    T_out* y = reinterpret_cast<T_out*>(p.Y);
+    ok = ptx::mbar_wait(acc_full, 0);
+    if (!__all_sync(0xffffffffu, ok) && lane == 0) atomicOr(&p.flags[FLAG_TIMEOUT], 1u);
+    ptx::tc_fence_after();
+    float* part = reinterpret_cast<float*>(sm) + row;            // [token][128 rows], where the ring was
+    for (int c0 = 0; c0 < valid; c0 += 16) {
+      uint32_t v[16];
+      ptx::tmem_ld_32x32b_x16(tmem + ((q * 32u) << 16) + (uint32_t)c0, v);
+      ptx::tmem_ld_wait();
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        if (ks > 1) part[(size_t)(c0 + j) * ROWS] = __uint_as_float(v[j]);
+        else if (c0 + j < valid && n < p.N) {
+          const float f = FMT == SDQ_FMT_NVFP4 ? fw * __ldg(p.fx + m0 + c0 + j) : 1.0f;
+          y[(m0 + c0 + j) * p.ldy + n] = to_out<DT>(fmaf(__uint_as_float(v[j]), f, b));
+        }
+      }
+    }
+    ptx::tc_fence_before();
+  }
+  if (ks > 1) {
+    ptx::cluster_sync();                                         // every CTA's partial tile is in place
+    if (warp >= 2) {
+      const uint32_t row = (warp & 3) * 32 + lane;
+      const int64_t n = (int64_t)nt * ROWS + row, m0 = (int64_t)mt * 128;
+      const int valid = (int)min((int64_t)T, p.M - m0);
+      float fw = 1.0f, b = 0.0f;
+      if (n < p.N) {
+        if (FMT == SDQ_FMT_NVFP4) fw = p.fw[n];
+        if (p.bias) b = from_out<DT>(reinterpret_cast<const T_out*>(p.bias)[n]);
+      }
+      T_out* y = reinterpret_cast<T_out*>(p.Y);
+      for (int c = (int)rank; c < valid; c += (int)ks) {
+        const float s = sum_over_cluster(ptx::smem_u32(sm) + (uint32_t)(c * ROWS + (int)row) * 4u, ks);
+        if (n < p.N) {
+          const float f = FMT == SDQ_FMT_NVFP4 ? fw * __ldg(p.fx + m0 + c) : 1.0f;
+          y[(m0 + c) * p.ldy + n] = to_out<DT>(fmaf(s, f, b));
+        }
+      }
+    }
+    ptx::cluster_sync();                                         // nobody leaves while its partial tile is being read
+  } else {
+    __syncthreads();
+  }
+  if (warp == 1) ptx::tmem_dealloc(tmem, 256);
+}
+
+// ---- many tokens ----------------------------------------------------------------------------------------------------------
+constexpr int WIDE_THREADS = 384;                    // producer, MMA issuer (odd CTA: forwarder), two idle, eight epilogue warps
+constexpr int WIDE_SLOTS = 5, WIDE_PAIRS = 4;
+// slot = | token record (codes, scale atoms) | codes of 128 weight rows | scale atoms of both CTAs' weight rows |
+__host__ __device__ constexpr uint32_t wide_slot(int fmt) { return record(fmt) + CODES + 2 * atoms(fmt) * ATOM; }
+constexpr uint32_t WIDE_PITCH = 68;                  // bytes of a staged row of 64
+constexpr uint32_t WIDE_TAIL = 256u + 2u * 2u * 256u * 4u + 8u * 32u * WIDE_PITCH + 128u;
+
+template <int FMT, int DT, bool VEC>
+__global__ void __launch_bounds__(WIDE_THREADS)
+mx4_linear_wide_kernel(const __grid_constant__ GemmParams p)
+{
+  using T_out = typename Out<DT>::type;
+  constexpr uint32_t NA = atoms(FMT), REC = record(FMT), SLOT = wide_slot(FMT), SFA_SET = 4u * NA, SET = 12u * NA;
+  constexpr uint32_t SL_B = REC, SL_SF = REC + CODES;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* sm = smem_raw + ((128 - (ptx::smem_u32(smem_raw) & 127)) & 127);
+  const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  uint64_t* full = reinterpret_cast<uint64_t*>(sm + WIDE_SLOTS * SLOT);
+  uint64_t* empty = full + WIDE_SLOTS;               // [pair of stages % WIDE_PAIRS]: the MMAs that read them have completed
+  uint64_t* acc_full = empty + WIDE_PAIRS;
+  uint64_t* acc_empty = acc_full + 1;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 1);
+  volatile uint32_t* timed_out = tmem_slot + 1;
+  float* s_fac = reinterpret_cast<float*>(sm + WIDE_SLOTS * SLOT + 256);       // [task parity][factor, bias][256 weight rows]
+  uint8_t* s_out = reinterpret_cast<uint8_t*>(s_fac + 4 * 256);
+  const uint32_t rank = ptx::cluster_ctarank();
+  const int pair = (int)blockIdx.x >> 1, n_pairs = (int)gridDim.x >> 1;
+  const int my_tasks = p.tasks > pair ? (p.tasks - pair + n_pairs - 1) / n_pairs : 0;
+  const int KB = p.kb;
+
+  if (warp == 0 && lane == 0) {
+    ptx::griddep_launch_dependents();
+    for (int i = 0; i < WIDE_SLOTS; ++i) ptx::mbar_init(&full[i], rank == 0 ? 2 : 1);
+    for (int i = 0; i < WIDE_PAIRS; ++i) ptx::mbar_init(&empty[i], 1);
+    ptx::mbar_init(acc_full, 1);
+    ptx::mbar_init(acc_empty, 16);
+    *timed_out = 0u;
+    ptx::fence_barrier_init();
+  }
+  __syncwarp();
+  if (warp == 1) ptx::tmem_alloc_pair(tmem_slot, 512);
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::cluster_sync();
+  ptx::tc_fence_after();
+  const uint32_t tmem = *tmem_slot, sets = tmem + 256u;
+  ptx::griddep_wait();
+
+  // task -> tiles of 256: weight tiles vary fastest inside bands of eight token tiles
+  auto tile_of = [&](int task, int& mt, int& nt) {
+    const int band = 8 * p.pt_n, b = task / band, r = task - b * band, h = min(8, p.pt_m - 8 * b);
+    nt = r / h;
+    mt = 8 * b + r - nt * h;
+  };
+  bool ok = true;
+  if (warp == 0) {
+    if (lane == 0) {
+      int i = 0;                                     // stage, counted through the CTA's tasks
+      for (int t = 0; t < my_tasks && ok; ++t) {
+        int mt, nt;
+        tile_of(pair + t * n_pairs, mt, nt);
+        // (an odd number of tiles: the last one is taken twice, and stored once)
+        const uint8_t* xa = p.x + (size_t)min(2 * mt + (int)rank, p.m_tiles - 1) * KB * REC;
+        const uint8_t* w0 = p.w + (size_t)(2 * nt) * KB * REC;
+        const uint8_t* w1 = p.w + (size_t)min(2 * nt + 1, p.n_tiles - 1) * KB * REC;
+        const uint8_t* wb = rank ? w1 : w0;
+        for (int k = 0; k < KB; ++k, ++i) {
+          if (i >= WIDE_SLOTS) {
+            const uint32_t q = (uint32_t)(i - WIDE_SLOTS) >> 1;
+            if (!(ok = ptx::mbar_wait(&empty[q % WIDE_PAIRS], (q / WIDE_PAIRS) & 1u))) break;
+          }
+          const uint32_t s = (uint32_t)i % WIDE_SLOTS;
+          uint8_t* st = sm + (size_t)s * SLOT;
+          const size_t off = (size_t)k * REC;
+          ptx::mbar_expect_tx(&full[s], SLOT);
+          ptx::bulk_g2s(st, xa + off, REC, &full[s]);
+          ptx::bulk_g2s(st + SL_B, wb + off, CODES, &full[s]);
+          ptx::bulk_g2s(st + SL_SF, w0 + off + CODES, NA * ATOM, &full[s]);
+          ptx::bulk_g2s(st + SL_SF + NA * ATOM, w1 + off + CODES, NA * ATOM, &full[s]);
+        }
+      }
+      if (!ok) atomicOr(&p.flags[FLAG_TIMEOUT], 1u);
+    }
+    __syncwarp();
+  } else if (warp == 1 && rank == 1) {
+    if (lane == 0) {                                 // this CTA's part of a slot has landed: told to the leader
+      const int total = my_tasks * KB;
+      for (int i = 0; i < total && ok; ++i) {
+        const uint32_t s = (uint32_t)i % WIDE_SLOTS;
+        if (!(ok = ptx::mbar_wait(&full[s], ((uint32_t)i / WIDE_SLOTS) & 1u))) break;
+        ptx::mbar_arrive_remote(&full[s], 0);
+      }
+      if (!ok) atomicOr(&p.flags[FLAG_TIMEOUT], 1u);
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    if (lane == 0) {
+      const uint32_t id0 = ptx::idesc_block_scaled(256, 256, 1, false, 0, 0) ^ (FMT == SDQ_FMT_NVFP4 ? 1u << 23 : 0u);
+      const uint32_t id2 = ptx::idesc_block_scaled(256, 256, 1, false, 2, 2);
+      const int total = my_tasks * KB;
+      int i = 0;
+      for (int t = 0; t < my_tasks && ok; ++t) {
+        for (int k = 0; k < KB; ++k, ++i) {
+          const uint32_t s = (uint32_t)i % WIDE_SLOTS;
+          if (!(ok = ptx::mbar_wait(&full[s], ((uint32_t)i / WIDE_SLOTS) & 1u))) break;
+          if (k == 0 && t > 0 && !(ok = ptx::mbar_wait(acc_empty, (uint32_t)(t - 1) & 1u))) break;
+          ptx::tc_fence_after();
+          const uint32_t st = ptx::smem_u32(sm) + s * SLOT, sfa = sets + (i & 1) * SET, sfb = sfa + SFA_SET;
+          const uint64_t da = ptx::smem_desc(st, 128, 1024), db = ptx::smem_desc(st + SL_B, 128, 1024);
+          const uint64_t ca = ptx::smem_desc(st + CODES, 0, 128), cb = ptx::smem_desc(st + SL_SF, 0, 128);
+#pragma unroll
+          for (uint32_t a = 0; a < NA; ++a) {
+            ptx::tc2_cp_32x128b_warpx4(sfa + 4 * a, ca + a * (ATOM >> 4));
+            ptx::tc2_cp_32x128b_warpx4(sfb + 8 * a, cb + a * (ATOM >> 4));
+            ptx::tc2_cp_32x128b_warpx4(sfb + 8 * a + 4, cb + (NA + a) * (ATOM >> 4));
+          }
+#pragma unroll
+          for (uint32_t j = 0; j < 4; ++j) {
+            const uint32_t acc = k || j ? 1u : 0u;
+            if constexpr (FMT == SDQ_FMT_NVFP4) ptx::mma2_nvf4(tmem, da + ((256 * j) >> 4), db + ((256 * j) >> 4), id0, sfa + 4 * j, sfb + 8 * j, acc);
+            else ptx::mma2_mxf4(tmem, da + ((256 * j) >> 4), db + ((256 * j) >> 4), j & 1 ? id2 : id0, sfa + 4 * (j >> 1), sfb + 8 * (j >> 1), acc);
+          }
+          // one release for two stages: a pair-wide commit costs the tensor pipe a bubble
+          if ((i & 1) && i + 1 < total) ptx::tc2_commit_both(&empty[(uint32_t)(i >> 1) % WIDE_PAIRS], 3);
+          if (k == KB - 1) ptx::tc2_commit_both(acc_full, 3);
+        }
+      }
+      if (!ok) atomicOr(&p.flags[FLAG_TIMEOUT], 1u);
+    }
+    __syncwarp();
+  } else if (warp >= 4) {
+    // epilogue: warp w owns TMEM lanes 32 (w % 4) .. (tokens); warps 4 to 7 the first 128 weight rows, 8 to 11 the others.  The
+    // accumulator is packed into registers and handed back before anything is stored.
+    const uint32_t q = warp & 3, half = (warp - 4) >> 2, et = tid - 128;
+    for (int t = 0; t < my_tasks && ok; ++t) {
+      int mt, nt;
+      tile_of(pair + t * n_pairs, mt, nt);
+      const int64_t n0 = (int64_t)nt * 256;
+      float* fac = s_fac + (t & 1) * 512;
+      {
+        const int64_t n = n0 + et;
+        fac[et] = FMT == SDQ_FMT_NVFP4 && n < p.N ? __ldg(p.fw + n) : 1.0f;
+        fac[256 + et] = p.bias && n < p.N ? from_out<DT>(reinterpret_cast<const T_out*>(p.bias)[n]) : 0.0f;
+      }
+      const int64_t m = (int64_t)(2 * mt + (int)rank) * ROWS + q * 32 + lane;
+      const float fx = FMT == SDQ_FMT_NVFP4 && m < p.M ? __ldg(p.fx + m) : 1.0f;
+      if (et == 0 && !ptx::mbar_wait(acc_full, (uint32_t)t & 1u)) *timed_out = 1u;
+      ptx::named_bar_sync(1, 256);
+      if (*timed_out) { ok = false; break; }
+      ptx::tc_fence_after();
+      constexpr int PER = DT == SDQ_FP32 ? 1 : 2, WORDS = 128 / PER;
+      uint32_t out[WORDS];
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        uint32_t v[16];
+        ptx::tmem_ld_32x32b_x16(tmem + ((q * 32u) << 16) + half * 128u + 16u * c, v);
+        ptx::tmem_ld_wait();
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const uint32_t col = half * 128u + 16u * c + j;
+          v[j] = __float_as_uint(fmaf(__uint_as_float(v[j]), FMT == SDQ_FMT_NVFP4 ? fac[col] * fx : 1.0f, fac[256 + col]));
+        }
+#pragma unroll
+        for (int j = 0; j < 16 / PER; ++j) {
+          if constexpr (DT == SDQ_FP32) out[16 * c + j] = v[j];
+          else if constexpr (DT == SDQ_BF16) {
+            const __nv_bfloat162 b = __floats2bfloat162_rn(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]));
+            out[8 * c + j] = *reinterpret_cast<const uint32_t*>(&b);
+          } else {
+            const __half2 b = __floats2half2_rn(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]));
+            out[8 * c + j] = *reinterpret_cast<const uint32_t*>(&b);
+          }
+        }
+      }
+      ptx::tc_fence_before();
+      __syncwarp();
+      if (lane == 0) { if (rank == 0) ptx::mbar_arrive(acc_empty); else ptx::mbar_arrive_remote(acc_empty, 0); }
+      if (2 * mt + (int)rank >= p.m_tiles) continue;             // (the repeated last tile)
+      T_out* y = reinterpret_cast<T_out*>(p.Y) + m * p.ldy + n0 + half * 128;
+      const int cols = (int)min((int64_t)128, p.N - n0 - (int64_t)half * 128);
+      if constexpr (VEC) {
+        if (m < p.M) {
+#pragma unroll
+          for (int c = 0; c < WORDS / 8; ++c) {                  // 32 bytes, one sector, a store
+            constexpr int EL = 8 * PER;
+            if ((c + 1) * EL <= cols)
+              asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(y + c * EL), "r"(out[8 * c]), "r"(out[8 * c + 1]), "r"(out[8 * c + 2]),
+                           "r"(out[8 * c + 3]), "r"(out[8 * c + 4]), "r"(out[8 * c + 5]), "r"(out[8 * c + 6]), "r"(out[8 * c + 7]) : "memory");
+          }
+        }
+      } else {
+        // any alignment: 64 bytes of 32 tokens at a time turned in shared memory, consecutive lanes store consecutive outputs of a token
+        constexpr int EL = 16 * PER, RUN = 32 / EL;              // outputs of a token at a time, tokens a store instruction covers
+        uint8_t* st = s_out + (warp - 4) * 32u * WIDE_PITCH;
+        const int64_t mw = m - lane;
+        const int rows = (int)min((int64_t)32, p.M - mw), col = (int)lane % EL, r0 = (int)lane / EL;
+#pragma unroll
+        for (int c = 0; c < WORDS / 16; ++c) {
+          __syncwarp();
+#pragma unroll
+          for (int j = 0; j < 16; ++j) *reinterpret_cast<uint32_t*>(st + lane * WIDE_PITCH + 4u * j) = out[16 * c + j];
+          __syncwarp();
+          if (c * EL + col < cols) {
+            T_out* yr = reinterpret_cast<T_out*>(p.Y) + mw * p.ldy + n0 + half * 128 + c * EL + col;
+            for (int r = r0; r < rows; r += RUN) yr[(int64_t)r * p.ldy] = *reinterpret_cast<const T_out*>(st + r * WIDE_PITCH + col * sizeof(T_out));
+          }
+        }
+      }
+    }
+    __syncwarp();
+  }
+  // (a peer may still signal barriers of this CTA, and its MMAs read this CTA's shared memory)
+  ptx::tc_fence_before();
+  __syncwarp();
+  ptx::cluster_sync();
+  if (warp == 1) ptx::tmem_dealloc_pair(tmem, 512);
+}
+
+// ---- launches ---------------------------------------------------------------------------------------------------------------
+template <typename K>
+static cudaError_t with_smem(K kern, uint32_t bytes, DeviceInfo* d, int bit) {
+  if (d->mx4_attr & (1u << bit)) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute((const void*)kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  if (e == cudaSuccess) d->mx4_attr |= 1u << bit;
+  return e;
+}
+constexpr uint32_t SMEM_MAX = 232448;
+
+template <int FMT, int DT>
+static sdq_status_t linear(GemmParams& p, DeviceInfo* d, void* stream) {
+  cudaLaunchConfig_t lc = {};
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  lc.attrs = attr;
+  lc.numAttrs = 2;
+  lc.stream = (cudaStream_t)stream;
+  constexpr int BIT = 3 * (FMT * 3 + DT);
+  if (p.M <= 512) {
+    p.T = p.M <= 128 ? (int32_t)(p.M + 15) / 16 * 16 : 128;
+    const int64_t tiles = (int64_t)p.n_tiles * p.m_tiles;
+    int ks = 1;
+    while (ks < 8 && 2 * ks * tiles <= 2 * d->sm_count && 2 * ks <= p.kb) ks *= 2;
+    const uint32_t slot = narrow_slot(FMT, p.T);
+    const uint32_t room = (tiles * ks <= d->sm_count ? SMEM_MAX : SMEM_MAX / 2 - 1024) - NARROW_TAIL;
+    const int want = (p.kb + ks - 1) / ks;
+    p.nslot = (int32_t)(room / slot);
+    if (p.nslot > want) p.nslot = want;
+    if (p.nslot > NARROW_MAX_SLOTS) p.nslot = NARROW_MAX_SLOTS;
+    if (p.n_tiles > 0x7FFFFFFF / 8 || p.m_tiles > 65535) return SDQ_ERR_SHAPE;
+    const uint32_t ring = (uint32_t)p.nslot * slot, parts = ks > 1 ? (uint32_t)p.T * ROWS * 4u : 0u;
+    // (the partial tile lies where the ring was; the barriers behind both)
+    if (parts > ring) p.nslot = (int32_t)((parts + slot - 1) / slot);
+    lc.gridDim = dim3((unsigned)(p.n_tiles * ks), (unsigned)p.m_tiles);
+    lc.blockDim = dim3(NARROW_THREADS);
+    // At least 80 KB: never more than two on an SM, as many as its tensor memory serves.  With a third, CTAs of two clusters could each hold
+    // the columns that the other's peer waits for
+    lc.dynamicSmemBytes = (uint32_t)p.nslot * slot + NARROW_TAIL > 81920u ? (uint32_t)p.nslot * slot + NARROW_TAIL : 81920u;
+    attr[1].val.clusterDim.x = (unsigned)ks;
+    auto kern = mx4_linear_narrow_kernel<FMT, DT>;
+    if (with_smem(kern, SMEM_MAX, d, BIT) != cudaSuccess) return launch_status(cudaErrorUnknown);
+    return launch_status(cudaLaunchKernelEx(&lc, kern, p));
+  }
+  p.pt_m = (p.m_tiles + 1) / 2;
+  p.pt_n = (p.n_tiles + 1) / 2;
+  if ((int64_t)p.pt_m * p.pt_n > 0x3FFFFFFF) return SDQ_ERR_SHAPE;
+  p.tasks = p.pt_m * p.pt_n;
+  const int pairs = d->sm_count / 2 < p.tasks ? d->sm_count / 2 : p.tasks;
+  lc.gridDim = dim3(2 * (unsigned)pairs);
+  lc.blockDim = dim3(WIDE_THREADS);
+  lc.dynamicSmemBytes = WIDE_SLOTS * wide_slot(FMT) + WIDE_TAIL;
+  static_assert(WIDE_SLOTS * wide_slot(FMT) + WIDE_TAIL <= SMEM_MAX, "the ring fits");
+  attr[1].val.clusterDim.x = 2;
+  const int64_t sector = 32 / (int64_t)dtype_bytes(DT);
+  const bool vec = ((uintptr_t)p.Y & 31) == 0 && p.ldy % sector == 0 && p.N % sector == 0;
+  auto go = [&](auto kern, int bit) {
+    if (with_smem(kern, lc.dynamicSmemBytes, d, bit) != cudaSuccess) return launch_status(cudaErrorUnknown);
+    return launch_status(cudaLaunchKernelEx(&lc, kern, p));
+  };
+  return vec ? go(mx4_linear_wide_kernel<FMT, DT, true>, BIT + 1) : go(mx4_linear_wide_kernel<FMT, DT, false>, BIT + 2);
+}
+
+}  // namespace mx4
+}  // namespace sdq
+
+using namespace sdq;
+
+extern "C" sdq_status_t sdq_mx4_linear(const sdq_mx4_t* Xq, const sdq_mx4_t* Wq, const void* bias, int32_t dtype, void* Y, int64_t ldy, void* stream)
+{
+  if (!mx4::desc_ok(Xq) || !mx4::desc_ok(Wq) || !Y || !mx4::dtype_ok(dtype)) return SDQ_ERR_INVALID_ARG;
+  if (Xq->E || Wq->E || Xq->fmt != Wq->fmt) return SDQ_ERR_UNSUPPORTED;
+  if (Xq->K != Wq->K || ldy < Wq->R || ldy > ((int64_t)1 << 40)) return SDQ_ERR_SHAPE;
+  const size_t es = mx4::dtype_bytes(dtype);
+  if (((uintptr_t)Y % es) || ((uintptr_t)bias % es)) return SDQ_ERR_ALIGNMENT;
+  const mx4::Dims dx = mx4::dims(0, Xq->R, Xq->K, Xq->fmt), dw = mx4::dims(0, Wq->R, Wq->K, Wq->fmt);
+  if (dx.tiles > 0x3FFFFFFF || dw.tiles > 0x3FFFFFFF) return SDQ_ERR_SHAPE;
+  DeviceInfo* d = device_info();
+  mx4::GemmParams p = {};
+  p.flags = device_flags();
+  if (!d || !p.flags) return SDQ_ERR_CUDA;
+  p.x = (const uint8_t*)Xq->dev; p.w = (const uint8_t*)Wq->dev;
+  p.fx = reinterpret_cast<const float*>(p.x + dx.off2); p.fw = reinterpret_cast<const float*>(p.w + dw.off2);
+  p.bias = bias; p.Y = Y; p.M = Xq->R; p.N = Wq->R; p.ldy = ldy;
+  p.kb = (int32_t)dx.kblocks; p.m_tiles = (int32_t)dx.tiles; p.n_tiles = (int32_t)dw.tiles;
+  auto go = [&](auto fmt) -> sdq_status_t {
+    constexpr int F = decltype(fmt)::value;
+    return dtype == SDQ_BF16   ? mx4::linear<F, SDQ_BF16>(p, d, stream)
+           : dtype == SDQ_FP16 ? mx4::linear<F, SDQ_FP16>(p, d, stream)
+                               : mx4::linear<F, SDQ_FP32>(p, d, stream);
+  };
+  return Xq->fmt == SDQ_FMT_NVFP4 ? go(std::integral_constant<int, SDQ_FMT_NVFP4>{}) : go(std::integral_constant<int, SDQ_FMT_MXFP4>{});
+}
