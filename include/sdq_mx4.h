@@ -27,6 +27,7 @@ extern "C" {
 
 enum { SDQ_FMT_MXFP4 = 0, SDQ_FMT_NVFP4 = 1 };
 enum { SDQ_BF16 = 0, SDQ_FP16 = 1, SDQ_FP32 = 2 };            /* element types of unquantized operands */
+enum { SDQ_ROUTE_SOFTMAX = 0, SDQ_ROUTE_SIGMOID = 1 };
 
 /* Host-side descriptor of a quantized matrix, or of the stacked matrices of E experts (plain data, may be copied; `dev`
  * stays owned by the caller).  off: 0 records (linear) / codes (experts)  1 scales (experts)  2 row factors (NVFP4) */
@@ -71,6 +72,26 @@ sdq_status_t sdq_mx4_experts_quantize(const void* W, int32_t dtype, int64_t E, i
                                       void* buf, size_t bytes, sdq_mx4_t* out, void* stream);
 sdq_status_t sdq_mx4_experts_import(const uint8_t* codes, const uint8_t* scales, int64_t E, int64_t R, int64_t K,
                                     void* buf, size_t bytes, sdq_mx4_t* out, void* stream);
+
+/* Router: logits = X Wr^T over the H channels, X [T][ldx] and Wr [E][ldw] of `dtype`; score = softmax over the E experts or
+ * sigmoid; every token's k experts are those of the largest score + bias (bias (device) [E] fp32 or NULL; of equal ones the lowest
+ * index first), in descending order; weight = score of the chosen, divided by their sum where `renorm`, times `scale`.
+ * Logits, scores and choices are formed in 64 bits from fp32 partial sums.  ids (device) [T][k] int32, weights (device) [T][k] fp32.
+ * 1 <= k <= E <= 1024, k <= 32. */
+sdq_status_t sdq_moe_route(const void* X, int32_t dtype, int64_t T, int64_t H, int64_t ldx, const void* Wr, int64_t E, int64_t ldw,
+                           const float* bias, int32_t k, int32_t scoring, int32_t renorm, float scale,
+                           int32_t* ids, float* weights, void* stream);
+
+/* Experts: Y[t] = sum_j weights[t][j] * W2[e](silu(W1[e] x_t) * W3[e] x_t), e = ids[t][j].  X [T][ldx], Y [T][ldy] bf16 or fp16;
+ * w1, w3 [E, I, H], w2 [E, H, I] in the experts' layout.  The activations are not quantized: the tensor core multiplies the 4-bit weights by
+ * E4M3 pieces whose sum is x (bf16: two, fp16: three) and silu(.) * (.) (three).  A pair whose id lies outside [0, E) adds
+ * nothing.  1 <= T <= 64, 1 <= k <= 32.  A token that holds an infinity or a NaN gives NaN.
+ * ws (device): scratch of sdq_mx4_moe_workspace_size bytes, needs no initialisation; calls that can overlap on the GPU must not
+ * share it. */
+sdq_status_t sdq_mx4_moe_workspace_size(int64_t T, int32_t k, int64_t H, int64_t I, size_t* bytes);
+sdq_status_t sdq_mx4_moe(const void* X, int32_t dtype, int64_t T, int64_t H, int64_t ldx, const int32_t* ids, const float* weights, int32_t k,
+                         const sdq_mx4_t* w1, const sdq_mx4_t* w3, const sdq_mx4_t* w2, void* Y, int64_t ldy,
+                         void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

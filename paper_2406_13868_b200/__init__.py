@@ -31,6 +31,7 @@ def gran_keep(n: int) -> int:
 SCALE_OCP_FLOOR, SCALE_CEIL_NOSAT, SCALE_UE4M3 = 0, 1, 2
 ORDER_LARGE, ORDER_SMALL = 0, 1
 OUT_E4M3, OUT_INT8 = 0, 1
+ROUTE_SOFTMAX, ROUTE_SIGMOID = 0, 1
 FMT_MXFP4, FMT_NVFP4 = 0, 1                 # plain microscaled formats: E8M0 scale per 32, E4M3 scale per 16 under a row factor
 
 STATUS = ["ok", "invalid_arg", "shape", "alignment", "unsupported", "buffer_too_small", "nonfinite", "cuda", "timeout"]
@@ -77,7 +78,8 @@ class _Mx4(ctypes.Structure):
 EXPORTS = ["sdq_packed_size", "sdq_decompose", "sdq_decompose_metric", "sdq_channel_norm", "sdq_packed_export", "sdq_packed_attach", "sdq_packed_compact_size", "sdq_packed_compact", "sdq_act_size", "sdq_quantize_act", "sdq_act_export",
            "sdq_linear", "sdq_linear_f32", "sdq_workspace_size", "sdq_workspace_init", "sdq_linear_ws", "sdq_linear_f32_ws", "sdq_linear_noalloc",
            "sdq_linear_group", "sdq_linear_group_f32", "sdq_linear_group_x", "sdq_linear_group_x_f32", "sdq_linear_group_x_ws", "sdq_linear_group_x_f32_ws", "sdq_mx4_size", "sdq_mx4_quantize", "sdq_mx4_import", "sdq_mx4_export", "sdq_mx4_dequantize", "sdq_mx4_linear",
-           "sdq_mx4_experts_size", "sdq_mx4_experts_quantize", "sdq_mx4_experts_import", "sdq_diag_l2_copy", "sdq_diag_wait_timeout", "sdq_diag_decompose_timeout", "sdq_diag_linear_plan", "sdq_diag_linear_rings", "sdq_diag_group_plan", "sdq_device_status", "sdq_status_string"]
+           "sdq_mx4_experts_size", "sdq_mx4_experts_quantize", "sdq_mx4_experts_import",
+           "sdq_moe_route", "sdq_mx4_moe_workspace_size", "sdq_mx4_moe", "sdq_diag_l2_copy", "sdq_diag_wait_timeout", "sdq_diag_decompose_timeout", "sdq_diag_linear_plan", "sdq_diag_linear_rings", "sdq_diag_group_plan", "sdq_device_status", "sdq_status_string"]
 
 _lib = None
 
@@ -122,6 +124,9 @@ def lib() -> ctypes.CDLL:
         L.sdq_mx4_experts_size.argtypes = [i64, i64, i64, ctypes.POINTER(sz)]
         L.sdq_mx4_experts_quantize.argtypes = [vp, i32, i64, i64, i64, i32, vp, sz, m4, vp]
         L.sdq_mx4_experts_import.argtypes = [vp, vp, i64, i64, i64, vp, sz, m4, vp]
+        L.sdq_moe_route.argtypes = [vp, i32, i64, i64, i64, vp, i64, i64, vp, i32, i32, i32, ctypes.c_float, vp, vp, vp]
+        L.sdq_mx4_moe_workspace_size.argtypes = [i64, i32, i64, i64, ctypes.POINTER(sz)]
+        L.sdq_mx4_moe.argtypes = [vp, i32, i64, i64, i64, vp, vp, i32, m4, m4, m4, vp, i64, vp, sz, vp]
         L.sdq_device_status.argtypes = [vp]
         L.sdq_status_string.argtypes = [ctypes.c_int]
         L.sdq_status_string.restype = ctypes.c_char_p
@@ -611,6 +616,65 @@ def sdq_mx4_linear(xq: Mx4Matrix, wq: Mx4Matrix, bias: torch.Tensor | None = Non
             raise ValueError("out has shape %s, not %s" % (tuple(out.shape), (xq.R, wq.R)))
     _check(lib().sdq_mx4_linear(ctypes.byref(xq.desc), ctypes.byref(wq.desc), None if bias is None else bias.data_ptr(), _DTYPES[dtype], out.data_ptr(),
                                 _row_stride(out), _stream()), "sdq_mx4_linear")
+    return out
+
+
+def sdq_moe_route(X: torch.Tensor, router: torch.Tensor, k: int, bias: torch.Tensor | None = None, scoring: int = ROUTE_SOFTMAX, renorm: bool = True,
+                  scale: float = 1.0):
+    """X [T, H], router [E, H] (one type of bf16, fp16, fp32) -> (ids int32 [T, k], weights fp32 [T, k]): the k experts of the largest score
+    (softmax or sigmoid of X router^T) + bias (fp32 [E]), in descending order, and their scores, divided by their sum if `renorm`, times
+    `scale`."""
+    _operand(X, "X", _DTYPES, 2)
+    _operand(router, "router", (X.dtype,), 2)
+    T, H = X.shape
+    E = router.shape[0]
+    if router.shape[1] != H:
+        raise ValueError("router has %d channels, X %d" % (router.shape[1], H))
+    if bias is not None:
+        _operand(bias, "bias", (torch.float32,), 1, False)
+        if bias.shape[0] != E:
+            raise ValueError("bias has %d entries for %d experts" % (bias.shape[0], E))
+    ids = torch.empty((T, k), dtype=torch.int32, device=X.device)
+    weights = torch.empty((T, k), dtype=torch.float32, device=X.device)
+    _check(lib().sdq_moe_route(X.data_ptr(), _DTYPES[X.dtype], T, H, _row_stride(X), router.data_ptr(), E, _row_stride(router),
+                               None if bias is None else bias.data_ptr(), k, scoring, int(renorm), scale, ids.data_ptr(), weights.data_ptr(), _stream()),
+           "sdq_moe_route")
+    return ids, weights
+
+
+def mx4_moe_workspace(T: int, k: int, H: int, I: int, device) -> torch.Tensor:
+    """Scratch of sdq_mx4_moe for up to T tokens and k choices; calls that can overlap on the GPU must not share one."""
+    b = ctypes.c_size_t()
+    _check(lib().sdq_mx4_moe_workspace_size(T, k, H, I, ctypes.byref(b)), "sdq_mx4_moe_workspace_size")
+    return torch.empty(b.value, dtype=torch.uint8, device=device)
+
+
+def sdq_mx4_moe(X: torch.Tensor, ids: torch.Tensor, weights: torch.Tensor, w1: Mx4Experts, w3: Mx4Experts, w2: Mx4Experts,
+                out: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """Y[t] = sum_j weights[t, j] * W2[e](silu(W1[e] x_t) * W3[e] x_t), e = ids[t, j], for up to 64 tokens.  X [T, H] bf16 or fp16, ids int32 and
+    weights fp32 [T, k]; ids outside [0, E) add nothing.  `workspace` from mx4_moe_workspace (else allocated for the call)."""
+    _operand(X, "X", (torch.bfloat16, torch.float16), 2)
+    T, H = X.shape
+    _operand(ids, "ids", (torch.int32,), 2, False)
+    _operand(weights, "weights", (torch.float32,), 2, False)
+    if ids.shape[0] != T or weights.shape != ids.shape:
+        raise ValueError("ids %s and weights %s do not belong to %d tokens" % (tuple(ids.shape), tuple(weights.shape), T))
+    for n, w in (("w1", w1), ("w3", w3), ("w2", w2)):
+        _same_device(w, n)
+    k = ids.shape[1]
+    if out is None:
+        out = torch.empty((T, H), dtype=X.dtype, device=X.device)
+    else:
+        _operand(out, "out", (X.dtype,), 2)
+        if out.shape != X.shape:
+            raise ValueError("out has shape %s, not %s" % (tuple(out.shape), tuple(X.shape)))
+    if workspace is None:
+        workspace = mx4_moe_workspace(T, k, H, w1.R, X.device)
+    else:
+        _operand(workspace, "workspace", (torch.uint8,), 1, False)
+    _check(lib().sdq_mx4_moe(X.data_ptr(), _DTYPES[X.dtype], T, H, _row_stride(X), ids.data_ptr(), weights.data_ptr(), k, ctypes.byref(w1.desc),
+                             ctypes.byref(w3.desc), ctypes.byref(w2.desc), out.data_ptr(), _row_stride(out), workspace.data_ptr(), workspace.numel(), _stream()),
+           "sdq_mx4_moe")
     return out
 
 

@@ -110,3 +110,26 @@ def test_the_binding_refuses_what_it_cannot_pass_on(m):
         m.sdq_mx4_import(torch.zeros(4, 32, dtype=torch.uint8), torch.zeros(4, 2, dtype=torch.uint8))
     with pytest.raises(ValueError, match="CUDA"):
         m.sdq_mx4_experts(torch.zeros(2, 4, 64, dtype=torch.bfloat16))
+
+
+def test_router_and_expert_layer_refuse_before_they_launch(m):
+    L, P = m.lib(), 1 << 20
+    r = lambda x=P, dt=0, T=4, H=64, ldx=64, w=P, E=8, ldw=64, bias=None, k=2, sc=0: L.sdq_moe_route(x, dt, T, H, ldx, w, E, ldw, bias, k, sc, 1, 1.0, P, P, None)  # noqa: E731
+    assert r(x=None) == 1 and r(dt=3) == 1 and r(sc=2) == 1
+    assert r(k=0) == 2 and r(k=9) == 2 and r(E=1025) == 2 and r(E=64, k=33) == 2 and r(T=0) == 2 and r(ldx=63) == 2 and r(ldw=63) == 2
+    assert r(x=P + 1) == 3 and r(bias=P + 2) == 3
+    b = ctypes.c_size_t()
+    assert L.sdq_mx4_moe_workspace_size(64, 8, 4096, 11008, ctypes.byref(b)) == 0 and b.value > 0
+    need = b.value
+    for bad in ((65, 8, 64, 64), (0, 8, 64, 64), (1, 33, 64, 64), (1, 0, 64, 64), (1, 1, 0, 64), (1, 1, 64, 0)):
+        assert L.sdq_mx4_moe_workspace_size(*bad, ctypes.byref(b)) == 2
+    w1, w3, w2 = _desc(m, 8, 11008, 4096, 0), _desc(m, 8, 11008, 4096, 0), _desc(m, 8, 4096, 11008, 0)
+
+    def go(a=w1, c=w3, d=w2, T=64, dt=0, ldx=4096, ws=P, size=need, x=P):
+        return L.sdq_mx4_moe(x, dt, T, 4096, ldx, P, P, 8, ctypes.byref(a), ctypes.byref(c), ctypes.byref(d), P, 4096, ws, size, None)
+    assert go(size=need - 1) == 5
+    assert go(T=65) == 2 and go(ldx=4095) == 2
+    assert go(dt=2) == 1 and go(x=None) == 1 and go(ws=None) == 1
+    assert go(ws=P + 16) == 3 and go(x=P + 1) == 3
+    assert go(a=_desc(m, 8, 11008, 4095, 0)) == 2 and go(c=_desc(m, 7, 11008, 4096, 0)) == 2 and go(d=_desc(m, 8, 4097, 11008, 0)) == 2
+    assert go(a=_desc(m, 0, 11008, 4096, 0)) == 4
