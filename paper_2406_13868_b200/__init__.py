@@ -155,7 +155,7 @@ def _native():
             loader = importlib.machinery.ExtensionFileLoader("_binding", BINDING)
             mod = importlib.util.module_from_spec(importlib.util.spec_from_loader("_binding", loader))
             loader.exec_module(mod)
-            mod.bind(_Act, _Packed, Config, QuantAct, PackedWeight, SdqError)
+            mod.bind(_Act, _Packed, Config, QuantAct, PackedWeight, SdqError, _Mx4, Mx4Matrix, Mx4Experts)
         except ImportError as e:
             warnings.warn("the binding's native half does not load (%s): calls go through ctypes, 6 to 12 us slower each; "
                           "`python -c 'import __graft_entry__ as g; g.build()'` builds it for this torch" % e)
@@ -501,6 +501,9 @@ def mx4_size(R: int, K: int, fmt: int = FMT_MXFP4) -> int:
 
 def sdq_mx4_quantize(X: torch.Tensor, fmt: int = FMT_MXFP4, rule: int = SCALE_OCP_FLOOR, buf: torch.Tensor | None = None) -> Mx4Matrix:
     """X [R, K] (bf16, fp16 or fp32 CUDA tensor; any sizes, rows may be strided) -> MXFP4 or NVFP4, weights and activations alike."""
+    q = (_fast or _native()).mx4_quantize(X, fmt, rule, buf)
+    if q is not None:
+        return q
     _operand(X, "X", _DTYPES, 2)
     R, K = X.shape
     buf = _buffer(buf, mx4_size(R, K, fmt), X.device)
@@ -551,9 +554,13 @@ def mx4_export(q) -> dict:
 
 def sdq_mx4_dequantize(q, dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None) -> torch.Tensor:
     """The values an Mx4Matrix ([R, K]) or Mx4Experts ([E, R, K]) holds."""
-    _same_device(q, "q")
     if dtype not in _DTYPES:
         raise ValueError("no output of type %s" % dtype)
+    if out is None:
+        y = (_fast or _native()).mx4_dequantize(q, _DTYPES[dtype])
+        if y is not None:
+            return y
+    _same_device(q, "q")
     experts = isinstance(q, Mx4Experts)
     shape = (q.E, q.R, q.K) if experts else (q.R, q.K)
     if out is None:
@@ -599,11 +606,14 @@ def sdq_mx4_experts_import(codes: torch.Tensor, scales: torch.Tensor, K: int | N
 def sdq_mx4_linear(xq: Mx4Matrix, wq: Mx4Matrix, bias: torch.Tensor | None = None, out: torch.Tensor | None = None,
                    dtype: torch.dtype | None = None) -> torch.Tensor:
     """Y [M, N] = Xq Wq^T + bias, fp32 sums on the tensor core, rounded once to `dtype` (of `out` if that is given, else bf16)."""
-    _same_device(xq, "xq")
-    _same_device(wq, "wq")
     dtype = dtype or (out.dtype if out is not None else torch.bfloat16)
     if dtype not in _DTYPES:
         raise ValueError("no output of type %s" % dtype)
+    y = (_fast or _native()).mx4_linear(xq, wq, bias, out, _DTYPES[dtype])
+    if y is not None:
+        return y
+    _same_device(xq, "xq")
+    _same_device(wq, "wq")
     if bias is not None:
         _operand(bias, "bias", (dtype,), 1, False)
         if bias.shape[0] != wq.R:
@@ -624,6 +634,9 @@ def sdq_moe_route(X: torch.Tensor, router: torch.Tensor, k: int, bias: torch.Ten
     """X [T, H], router [E, H] (one type of bf16, fp16, fp32) -> (ids int32 [T, k], weights fp32 [T, k]): the k experts of the largest score
     (softmax or sigmoid of X router^T) + bias (fp32 [E]), in descending order, and their scores, divided by their sum if `renorm`, times
     `scale`."""
+    r = (_fast or _native()).moe_route(X, router, k, bias, scoring, renorm, float(scale))
+    if r is not None:
+        return r
     _operand(X, "X", _DTYPES, 2)
     _operand(router, "router", (X.dtype,), 2)
     T, H = X.shape
@@ -653,6 +666,9 @@ def sdq_mx4_moe(X: torch.Tensor, ids: torch.Tensor, weights: torch.Tensor, w1: M
                 out: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
     """Y[t] = sum_j weights[t, j] * W2[e](silu(W1[e] x_t) * W3[e] x_t), e = ids[t, j], for up to 64 tokens.  X [T, H] bf16 or fp16, ids int32 and
     weights fp32 [T, k]; ids outside [0, E) add nothing.  `workspace` from mx4_moe_workspace (else allocated for the call)."""
+    y = (_fast or _native()).mx4_moe(X, ids, weights, w1, w3, w2, out, workspace)
+    if y is not None:
+        return y
     _operand(X, "X", (torch.bfloat16, torch.float16), 2)
     T, H = X.shape
     _operand(ids, "ids", (torch.int32,), 2, False)

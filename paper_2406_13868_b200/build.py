@@ -34,7 +34,7 @@ def _binding_stale() -> bool:
     if not os.path.exists(BINDING):
         return True
     t = os.path.getmtime(BINDING)
-    return any(os.path.getmtime(os.path.join(CSRC, f)) > t for f in [BINDING_SOURCE, os.path.join("..", "..", "include", "sdq.h")])
+    return any(os.path.getmtime(os.path.join(CSRC, f)) > t for f in [BINDING_SOURCE, os.path.join("..", "..", "include", "sdq.h"), os.path.join("..", "..", "include", "sdq_mx4.h")])
 
 
 def _build_binding() -> None:

@@ -17,6 +17,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "../../include/sdq.h"
+#include "../../include/sdq_mx4.h"
 
 namespace {
 
@@ -26,6 +27,9 @@ PyTypeObject* config_type = nullptr;
 PyObject* quant_act = nullptr;           // class QuantAct
 PyObject* packed_weight = nullptr;       // class PackedWeight
 PyObject* sdq_error = nullptr;           // class SdqError
+PyTypeObject* mx4_type = nullptr;        // the ctypes structure of sdq_mx4_t
+PyObject* mx4_matrix = nullptr;          // class Mx4Matrix
+PyObject* mx4_experts = nullptr;         // class Mx4Experts
 PyObject *s_desc, *s_buf, *s_N, *s_K, *s_cfg, *s_algo;
 
 // memory of a ctypes structure, held for the lifetime of this object
@@ -83,11 +87,12 @@ at::Tensor new_output(int64_t M, int64_t N, at::ScalarType type, const at::Devic
 #define NOT_HERE Py_RETURN_NONE
 
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (n != 6 || !PyType_Check(a[0]) || !PyType_Check(a[1]) || !PyType_Check(a[2])) {
-    PyErr_SetString(PyExc_TypeError, "bind(Act, Packed, Config, QuantAct, PackedWeight, SdqError)");
+  if (n != 9 || !PyType_Check(a[0]) || !PyType_Check(a[1]) || !PyType_Check(a[2]) || !PyType_Check(a[6])) {
+    PyErr_SetString(PyExc_TypeError, "bind(Act, Packed, Config, QuantAct, PackedWeight, SdqError, Mx4, Mx4Matrix, Mx4Experts)");
     return nullptr;
   }
-  for (int i = 0; i < 6; ++i) Py_INCREF(a[i]);
+  for (int i = 0; i < 9; ++i) Py_INCREF(a[i]);
+  mx4_type = (PyTypeObject*)a[6]; mx4_matrix = a[7]; mx4_experts = a[8];
   act_type = (PyTypeObject*)a[0]; packed_type = (PyTypeObject*)a[1]; config_type = (PyTypeObject*)a[2];
   quant_act = a[3]; packed_weight = a[4]; sdq_error = a[5];
   Py_RETURN_NONE;
@@ -380,7 +385,217 @@ PyObject* channel_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
-PyMethodDef methods[] = {{"decompose", (PyCFunction)(void (*)(void))decompose, METH_FASTCALL, nullptr},
+// ---- plain microscaled 4-bit matrices and the expert layer (include/sdq_mx4.h) -------------------------------------------
+// element type as the C-ABI names it; -1: none of them
+int mx4_dtype(at::ScalarType t) { return t == at::kBFloat16 ? SDQ_BF16 : t == at::kHalf ? SDQ_FP16 : t == at::kFloat ? SDQ_FP32 : -1; }
+bool is_current(const at::Tensor& t) { return t.is_cuda() && t.device().index() == c10::cuda::current_device(); }
+// a matrix on the current device with dense rows that do not overlap, of the type, if one is given
+const at::Tensor* matrix(PyObject* o, int dtype = -1) {
+  if (!THPVariable_Check(o)) return nullptr;
+  const at::Tensor& t = THPVariable_Unpack(o);
+  const int d = mx4_dtype(t.scalar_type());
+  if (d < 0 || (dtype >= 0 && d != dtype) || t.dim() != 2 || !is_current(t) || (t.size(1) > 1 && t.stride(1) != 1) || (t.size(0) > 1 && t.stride(0) < t.size(1))) return nullptr;
+  return &t;
+}
+int64_t row_stride(const at::Tensor& t) { return t.size(0) > 1 ? t.stride(0) : t.size(1); }
+// a contiguous tensor of so many entries, dimensions and this type on the current device
+const at::Tensor* dense(PyObject* o, at::ScalarType type, int64_t dims) {
+  if (!THPVariable_Check(o)) return nullptr;
+  const at::Tensor& t = THPVariable_Unpack(o);
+  return t.scalar_type() == type && t.dim() == dims && is_current(t) && t.is_contiguous() ? &t : nullptr;
+}
+// descriptor and buffer of an Mx4Matrix or Mx4Experts on the current device
+struct Mx4 {
+  explicit Mx4(PyObject* o) : desc(attr(o, s_desc)), buf(attr(o, s_buf)) {
+    q = (const sdq_mx4_t*)view.open(desc.get(), mx4_type);
+    if (q && (!buf.get() || !THPVariable_Check(buf.get()) || !is_current(THPVariable_Unpack(buf.get())))) q = nullptr;
+  }
+  Ref desc, buf;
+  View view;
+  const sdq_mx4_t* q;
+};
+bool to_int(PyObject* o, int64_t& v) {
+  if (!PyLong_Check(o)) return false;
+  v = PyLong_AsLongLong(o);
+  if (v == -1 && PyErr_Occurred()) { PyErr_Clear(); return false; }
+  return v >= INT32_MIN && v <= INT32_MAX;
+}
+at::TensorOptions on(const at::Tensor& t, at::ScalarType type) { return at::TensorOptions().dtype(type).device(t.device()); }
+
+// mx4_quantize(X, fmt, rule, buf or None) -> Mx4Matrix
+PyObject* mx4_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  int64_t fmt, rule;
+  if (n != 4 || !to_int(a[1], fmt) || !to_int(a[2], rule)) NOT_HERE;
+  const at::Tensor* X = matrix(a[0]);
+  if (!X) NOT_HERE;
+  const int64_t R = X->size(0), K = X->size(1);
+  at::Tensor buf;
+  if (a[3] == Py_None) {
+    size_t bytes = 0;
+    const sdq_status_t st = sdq_mx4_size(R, K, (int32_t)fmt, &bytes);
+    if (st != SDQ_OK) return raise(st, "sdq_mx4_size");
+    buf = at::empty({(int64_t)bytes}, on(*X, at::kByte));
+  } else {
+    const at::Tensor* b = dense(a[3], at::kByte, 1);
+    if (!b) NOT_HERE;
+    buf = *b;
+  }
+  Ref desc(PyObject_CallNoArgs((PyObject*)mx4_type));
+  if (!desc.get()) return nullptr;
+  {
+    View vd;
+    sdq_mx4_t* d = (sdq_mx4_t*)vd.open(desc.get(), mx4_type);
+    if (!d) NOT_HERE;
+    void *stream = current_stream(), *x = X->data_ptr(), *b = buf.data_ptr();
+    const int64_t ld = row_stride(*X);
+    const size_t room = (size_t)buf.numel();
+    const int dt = mx4_dtype(X->scalar_type());
+    sdq_status_t st;
+    Py_BEGIN_ALLOW_THREADS
+    st = sdq_mx4_quantize(x, dt, R, K, ld, (int32_t)fmt, (int32_t)rule, b, room, d, stream);
+    Py_END_ALLOW_THREADS
+    if (st != SDQ_OK) return raise(st, "sdq_mx4_quantize");
+  }
+  Ref b(a[3] == Py_None ? THPVariable_Wrap(std::move(buf)) : Py_NewRef(a[3])), r(PyLong_FromLongLong(R)), k(PyLong_FromLongLong(K));
+  if (!b.get() || !r.get() || !k.get()) return nullptr;
+  PyObject* args[5] = {b.get(), desc.get(), r.get(), k.get(), a[1]};
+  return PyObject_Vectorcall(mx4_matrix, args, 5, nullptr);
+  END_HANDLE_TH_ERRORS
+}
+
+// mx4_linear(xq, wq, bias or None, out or None, dtype as the C-ABI names it) -> out
+PyObject* mx4_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  int64_t dt;
+  if (n != 5 || !to_int(a[4], dt) || dt < SDQ_BF16 || dt > SDQ_FP32) NOT_HERE;
+  Mx4 x(a[0]), w(a[1]);
+  if (!x.q || !w.q || x.q->E || w.q->E) NOT_HERE;
+  const at::ScalarType type = dt == SDQ_BF16 ? at::kBFloat16 : dt == SDQ_FP16 ? at::kHalf : at::kFloat;
+  const void* bias = nullptr;
+  if (a[2] != Py_None) {
+    const at::Tensor* b = dense(a[2], type, 1);
+    if (!b || b->size(0) != w.q->R) NOT_HERE;
+    bias = b->data_ptr();
+  }
+  at::Tensor out;
+  if (a[3] == Py_None) {
+    out = at::empty({x.q->R, w.q->R}, on(THPVariable_Unpack(w.buf.get()), type));
+  } else {
+    const at::Tensor* o = matrix(a[3], (int)dt);
+    if (!o || o->size(0) != x.q->R || o->size(1) != w.q->R) NOT_HERE;
+    out = *o;
+  }
+  void *y = out.data_ptr(), *stream = current_stream();
+  const int64_t ldy = row_stride(out);
+  sdq_status_t st;
+  Py_BEGIN_ALLOW_THREADS
+  st = sdq_mx4_linear(x.q, w.q, bias, (int32_t)dt, y, ldy, stream);
+  Py_END_ALLOW_THREADS
+  if (st != SDQ_OK) return raise(st, "sdq_mx4_linear");
+  return a[3] == Py_None ? THPVariable_Wrap(std::move(out)) : Py_NewRef(a[3]);
+  END_HANDLE_TH_ERRORS
+}
+
+// mx4_dequantize(q, dtype as the C-ABI names it) -> new [R, K] (experts: [E, R, K])
+PyObject* mx4_dequantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  int64_t dt;
+  if (n != 2 || !to_int(a[1], dt) || dt < SDQ_BF16 || dt > SDQ_FP32) NOT_HERE;
+  Mx4 q(a[0]);
+  if (!q.q) NOT_HERE;
+  const at::TensorOptions opt = on(THPVariable_Unpack(q.buf.get()), dt == SDQ_BF16 ? at::kBFloat16 : dt == SDQ_FP16 ? at::kHalf : at::kFloat);
+  at::Tensor out = q.q->E ? at::empty({q.q->E, q.q->R, q.q->K}, opt) : at::empty({q.q->R, q.q->K}, opt);
+  void *y = out.data_ptr(), *stream = current_stream();
+  sdq_status_t st;
+  Py_BEGIN_ALLOW_THREADS
+  st = sdq_mx4_dequantize(q.q, y, (int32_t)dt, q.q->K, stream);
+  Py_END_ALLOW_THREADS
+  if (st != SDQ_OK) return raise(st, "sdq_mx4_dequantize");
+  return THPVariable_Wrap(std::move(out));
+  END_HANDLE_TH_ERRORS
+}
+
+// moe_route(X, router, k, bias or None, scoring, renorm, scale) -> (ids, weights)
+PyObject* moe_route(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  int64_t k, scoring;
+  if (n != 7 || !to_int(a[2], k) || !to_int(a[4], scoring) || !PyFloat_Check(a[6])) NOT_HERE;
+  const int renorm = PyObject_IsTrue(a[5]);
+  if (renorm < 0) { PyErr_Clear(); NOT_HERE; }
+  const at::Tensor* X = matrix(a[0]);
+  if (!X || k < 1) NOT_HERE;
+  const int dt = mx4_dtype(X->scalar_type());
+  const at::Tensor* W = matrix(a[1], dt);
+  if (!W || W->size(1) != X->size(1)) NOT_HERE;
+  const float* bias = nullptr;
+  if (a[3] != Py_None) {
+    const at::Tensor* b = dense(a[3], at::kFloat, 1);
+    if (!b || b->size(0) != W->size(0)) NOT_HERE;
+    bias = (const float*)b->data_ptr();
+  }
+  const int64_t T = X->size(0), H = X->size(1), E = W->size(0);
+  at::Tensor ids = at::empty({T, k}, on(*X, at::kInt)), weights = at::empty({T, k}, on(*X, at::kFloat));
+  void *x = X->data_ptr(), *w = W->data_ptr(), *i = ids.data_ptr(), *v = weights.data_ptr(), *stream = current_stream();
+  const int64_t ldx = row_stride(*X), ldw = row_stride(*W);
+  const float scale = (float)PyFloat_AS_DOUBLE(a[6]);
+  sdq_status_t st;
+  Py_BEGIN_ALLOW_THREADS
+  st = sdq_moe_route(x, dt, T, H, ldx, w, E, ldw, bias, (int32_t)k, (int32_t)scoring, renorm, scale, (int32_t*)i, (float*)v, stream);
+  Py_END_ALLOW_THREADS
+  if (st != SDQ_OK) return raise(st, "sdq_moe_route");
+  Ref pi(THPVariable_Wrap(std::move(ids))), pw(THPVariable_Wrap(std::move(weights)));
+  return pi.get() && pw.get() ? PyTuple_Pack(2, pi.get(), pw.get()) : nullptr;
+  END_HANDLE_TH_ERRORS
+}
+
+// mx4_moe(X, ids, weights, w1, w3, w2, out or None, workspace or None) -> out
+PyObject* mx4_moe(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 8) NOT_HERE;
+  const at::Tensor *X = matrix(a[0]), *ids = dense(a[1], at::kInt, 2), *weights = dense(a[2], at::kFloat, 2);
+  if (!X || !ids || !weights || X->scalar_type() == at::kFloat) NOT_HERE;
+  const int64_t T = X->size(0), H = X->size(1), k = ids->size(1);
+  if (ids->size(0) != T || weights->size(0) != T || weights->size(1) != k || k > INT32_MAX) NOT_HERE;
+  Mx4 w1(a[3]), w3(a[4]), w2(a[5]);
+  if (!w1.q || !w3.q || !w2.q) NOT_HERE;
+  const int dt = mx4_dtype(X->scalar_type());
+  at::Tensor out, ws;
+  if (a[6] == Py_None) {
+    out = at::empty({T, H}, on(*X, X->scalar_type()));
+  } else {
+    const at::Tensor* o = matrix(a[6], dt);
+    if (!o || o->size(0) != T || o->size(1) != H) NOT_HERE;
+    out = *o;
+  }
+  if (a[7] == Py_None) {
+    size_t bytes = 0;
+    const sdq_status_t st = sdq_mx4_moe_workspace_size(T, (int32_t)k, H, w1.q->R, &bytes);
+    if (st != SDQ_OK) return raise(st, "sdq_mx4_moe_workspace_size");
+    ws = at::empty({(int64_t)bytes}, on(*X, at::kByte));
+  } else {
+    const at::Tensor* w = dense(a[7], at::kByte, 1);
+    if (!w) NOT_HERE;
+    ws = *w;
+  }
+  void *x = X->data_ptr(), *i = ids->data_ptr(), *v = weights->data_ptr(), *y = out.data_ptr(), *s = ws.data_ptr(), *stream = current_stream();
+  const int64_t ldx = row_stride(*X), ldy = row_stride(out);
+  const size_t room = (size_t)ws.numel();
+  sdq_status_t st;
+  Py_BEGIN_ALLOW_THREADS
+  st = sdq_mx4_moe(x, dt, T, H, ldx, (const int32_t*)i, (const float*)v, (int32_t)k, w1.q, w3.q, w2.q, y, ldy, s, room, stream);
+  Py_END_ALLOW_THREADS
+  if (st != SDQ_OK) return raise(st, "sdq_mx4_moe");
+  return a[6] == Py_None ? THPVariable_Wrap(std::move(out)) : Py_NewRef(a[6]);
+  END_HANDLE_TH_ERRORS
+}
+
+PyMethodDef methods[] = {{"mx4_quantize", (PyCFunction)(void (*)(void))mx4_quantize, METH_FASTCALL, nullptr},
+                         {"mx4_linear", (PyCFunction)(void (*)(void))mx4_linear, METH_FASTCALL, nullptr},
+                         {"mx4_dequantize", (PyCFunction)(void (*)(void))mx4_dequantize, METH_FASTCALL, nullptr},
+                         {"moe_route", (PyCFunction)(void (*)(void))moe_route, METH_FASTCALL, nullptr},
+                         {"mx4_moe", (PyCFunction)(void (*)(void))mx4_moe, METH_FASTCALL, nullptr},
+                         {"decompose", (PyCFunction)(void (*)(void))decompose, METH_FASTCALL, nullptr},
                          {"compact", (PyCFunction)(void (*)(void))compact, METH_FASTCALL, nullptr},
                          {"channel_norm", (PyCFunction)(void (*)(void))channel_norm, METH_FASTCALL, nullptr},
                          {"bind", (PyCFunction)(void (*)(void))bind, METH_FASTCALL, nullptr},

@@ -237,3 +237,45 @@ def test_route_and_experts_as_a_decoder_uses_them(m):
     torch.cuda.synchronize()
     assert all(torch.equal(o[0], want[i % 3][0]) and torch.equal(o[1], want[i % 3][1]) for i, o in enumerate(outs))
     assert m.device_status() == 0
+
+
+def test_without_the_native_half_the_calls_go_through_ctypes(m, monkeypatch):
+    """same results, same refusals, whichever half marshals"""
+    T, H, I, E, k = 5, 192, 130, 6, 2
+    g = torch.Generator().manual_seed(4)
+    x, router = torch.randn(T, H, generator=g).bfloat16().cuda(), torch.randn(E, H, generator=g).bfloat16().cuda()
+    (w1, _), (w3, _), (w2, _) = experts(m, E, I, H, 1), experts(m, E, I, H, 2), experts(m, E, H, I, 3)
+
+    def all_calls():
+        ids, w = m.sdq_moe_route(x, router, k, scale=1)
+        y = m.sdq_mx4_moe(x, ids, w, w1, w3, w2)
+        q = m.sdq_mx4_quantize(y, m.FMT_NVFP4)
+        v = m.sdq_mx4_dequantize(q, torch.float16)
+        return [ids, w, y, v, m.sdq_mx4_dequantize(w1, torch.float32), m.sdq_mx4_linear(q, q, bias=y[:, 0].contiguous()),
+                m.sdq_mx4_linear(q, q, out=torch.zeros(T, T, device="cuda"))]
+
+    def refusals():
+        for bad in (lambda: m.sdq_mx4_quantize(x.int()), lambda: m.sdq_mx4_quantize(x.t()), lambda: m.sdq_mx4_quantize(x[0]), lambda: m.sdq_mx4_quantize(x, buf=x),
+                    lambda: m.sdq_mx4_linear(m.sdq_mx4_quantize(x), m.sdq_mx4_quantize(x), bias=x[0]), lambda: m.sdq_mx4_quantize(x.expand(T, H).as_strided((T, H), (1, 1))),
+                    lambda: m.sdq_mx4_linear(m.sdq_mx4_quantize(x), m.sdq_mx4_quantize(x), out=torch.zeros(T, T + 1, device="cuda")),
+                    lambda: m.sdq_moe_route(x, router.float(), k), lambda: m.sdq_moe_route(x, router[:, 1:], k), lambda: m.sdq_moe_route(x, router, k, bias=x[0]),
+                    lambda: m.sdq_mx4_moe(x, torch.zeros(T, k, device="cuda"), torch.zeros(T, k, device="cuda"), w1, w3, w2),
+                    lambda: m.sdq_mx4_moe(x, torch.zeros(T, k, device="cuda").int(), torch.zeros(T, k + 1, device="cuda"), w1, w3, w2),
+                    lambda: m.sdq_mx4_moe(x.cpu(), torch.zeros(T, k, device="cuda").int(), torch.zeros(T, k, device="cuda"), w1, w3, w2)):
+            with pytest.raises(ValueError):
+                bad()
+        for bad in (lambda: m.sdq_mx4_quantize(x, 7), lambda: m.sdq_mx4_quantize(x, rule=m.SCALE_UE4M3), lambda: m.sdq_moe_route(x, router, E + 1),
+                    lambda: m.sdq_mx4_linear(m.sdq_mx4_quantize(x), m.sdq_mx4_quantize(x, m.FMT_NVFP4)), lambda: m.sdq_mx4_quantize(x[:0]),
+                    lambda: m.sdq_mx4_quantize(x, buf=torch.empty(1024, dtype=torch.uint8, device="cuda")),
+                    lambda: m.sdq_mx4_moe(x, torch.zeros(T, k, device="cuda").int(), torch.zeros(T, k, device="cuda"), w1, w3, w1),
+                    lambda: m.sdq_mx4_moe(x, torch.zeros(T, k, device="cuda").int(), torch.zeros(T, k, device="cuda"), w1, w3, w2,
+                                          workspace=torch.empty(1024, dtype=torch.uint8, device="cuda"))):
+            with pytest.raises(m.SdqError):
+                bad()
+
+    want = all_calls()
+    refusals()
+    monkeypatch.setattr(m, "_fast", m._NoNative())
+    for a, b in zip(all_calls(), want):
+        assert a.dtype == b.dtype and torch.equal(a, b)
+    refusals()
