@@ -32,8 +32,31 @@ def test_no_remote_shared_memory_before_the_cluster_has_started(bodies):
 
 
 def test_global_memory_is_read_behind_the_wait_for_the_launch_in_front(bodies):
-    """every kernel lets the next launch in at once, so each waits before its first copy; only a prefetch into L2 may come earlier"""
+    """every kernel that lets the next launch in at once waits before its first copy; only a prefetch into L2 may come earlier"""
     for n, b in bodies.items():
+        if n in ("moe_up_kernel", "moe_down_kernel"):
+            continue
         wait = b.index("ptx::griddep_wait()")
         for what in (r"ptx::bulk_g2s\(", r"__ldg\(", r"\bload_unit<", r"get_codes<", r"put_codes<", r"codes\[r", r"atomicOr\(", r"\bload8<", r"load_tile\(", r"p\.(?:ids|weights|ws)\b"):
             assert all(x.start() > wait for x in re.finditer(what, b)), (n, what)
+
+
+def test_expert_layer_reads_ids_and_weights_early_only_behind_launches_that_have_waited(bodies):
+    """the products read ids and expert weights in front of their own wait, so the launches in front of them, the layer's own, let them in
+    behind theirs; the scratch, the tokens and the outputs are touched behind the wait"""
+    for n in ("moe_split_kernel", "moe_up_kernel", "moe_down_kernel"):
+        b = bodies[n]
+        lets_in = [x.start() for x in re.finditer(r"griddep_launch_dependents\(\)", b)]
+        assert len(lets_in) == 1
+        assert re.search(r"ptx::griddep_wait\(\);\s*if \((?:lane|tid) == 0\) $", b[:lets_in[0] - len("ptx::")])
+    for n in ("moe_up_kernel", "moe_down_kernel"):
+        b = bodies[n]
+        roles = re.split(r"\} else if \(warp", b[b.index("bool ok = true"):])
+        assert sum("p.ws" in r for r in roles) == 2
+        for r in roles:
+            if "p.ws" in r:
+                assert r.index("ptx::griddep_wait()") < r.index("p.ws")
+            if "p.weights" in r:
+                assert r.index("ptx::griddep_wait()") < r.index("p.weights")
+    tail = bodies["moe_down_kernel"]
+    assert tail.rindex("ptx::griddep_wait()") < tail.index("p.y")
