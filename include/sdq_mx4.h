@@ -30,14 +30,14 @@ enum { SDQ_BF16 = 0, SDQ_FP16 = 1, SDQ_FP32 = 2 };            /* element types o
 enum { SDQ_ROUTE_SOFTMAX = 0, SDQ_ROUTE_SIGMOID = 1 };
 
 /* Host-side descriptor of a quantized matrix, or of the stacked matrices of E experts (plain data, may be copied; `dev`
- * stays owned by the caller).  off: 0 records (linear) / codes (experts)  1 scales (experts)  2 row factors (NVFP4) */
+ * stays owned by the caller) */
 typedef struct {
   void* dev;
   size_t bytes;
   int64_t E, R, K;      /* E = 0: a linear matrix [R, K]; else E matrices [R, K] in the experts' layout */
   int32_t fmt;
   int32_t reserved;
-  size_t off[3];
+  size_t factors;       /* byte offset of the row factors (NVFP4) */
 } sdq_mx4_t;
 
 /* Bytes of the buffer of an R x K matrix. */
@@ -84,8 +84,9 @@ sdq_status_t sdq_moe_route(const void* X, int32_t dtype, int64_t T, int64_t H, i
 
 /* Experts: Y[t] = sum_j weights[t][j] * W2[e](silu(W1[e] x_t) * W3[e] x_t), e = ids[t][j].  X [T][ldx], Y [T][ldy] bf16 or fp16;
  * w1, w3 [E, I, H], w2 [E, H, I] in the experts' layout.  The activations are not quantized: the tensor core multiplies the 4-bit weights by
- * E4M3 pieces whose sum is x (bf16: two, fp16: three) and silu(.) * (.) (three).  A pair whose id lies outside [0, E) adds
- * nothing.  1 <= T <= 64, 1 <= k <= 32.  A token that holds an infinity or a NaN gives NaN.
+ * six E2M1 pieces whose sum is x, exactly down to 2^-9 (fp16: 2^-6) of the largest magnitude of its 32 channels and to 2^-17 of that
+ * below; the same for silu(.) * (.) in fp32.  A pair whose id lies outside [0, E) adds nothing.  1 <= T <= 64, 1 <= k <= 32.  A token that
+ * holds an infinity or a NaN gives NaN.
  * ws (device): scratch of sdq_mx4_moe_workspace_size bytes, needs no initialisation; calls that can overlap on the GPU must not
  * share it. */
 sdq_status_t sdq_mx4_moe_workspace_size(int64_t T, int32_t k, int64_t H, int64_t I, size_t* bytes);

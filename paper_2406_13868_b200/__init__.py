@@ -72,7 +72,7 @@ class _ActCanon(ctypes.Structure):
 
 class _Mx4(ctypes.Structure):
     _fields_ = [("dev", ctypes.c_void_p), ("bytes", ctypes.c_size_t), ("E", ctypes.c_int64), ("R", ctypes.c_int64), ("K", ctypes.c_int64),
-                ("fmt", ctypes.c_int32), ("reserved", ctypes.c_int32), ("off", ctypes.c_size_t * 3)]
+                ("fmt", ctypes.c_int32), ("reserved", ctypes.c_int32), ("factors", ctypes.c_size_t)]
 
 
 EXPORTS = ["sdq_packed_size", "sdq_decompose", "sdq_decompose_metric", "sdq_channel_norm", "sdq_packed_export", "sdq_packed_attach", "sdq_packed_compact_size", "sdq_packed_compact", "sdq_act_size", "sdq_quantize_act", "sdq_act_export",

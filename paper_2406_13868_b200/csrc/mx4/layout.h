@@ -8,12 +8,10 @@
 //          MXFP4: 128 K an atom, NVFP4: 64 K
 // K is padded to 256 with codes and scales of zero; rows behind R are not written (they only reach outputs that are not stored).
 //
-// Experts' form (MXFP4).  Every expert's rows in tiles of 128, K in steps of 128; codes 8192 B per (expert, row tile, step):
-//   row r, byte b of its 64 at (r/8)*512 + (b/8)*64 + (r%8)*8 + b%8: the core matrices of 8 rows x 16 elements that the 8-bit kind with 4-bit
-//   operands reads, without the padding the copy to shared memory inserts (8 bytes behind every 8).  128 elements, one core matrix, are one
-//   row of the tensor map that copies them.
-// scales: a section of their own, one atom (four scales of 32 K) per (expert, row tile, step).  Rows are padded to 128 and K
-// to 128 with zeros: a padded row of a gate is a zero of what follows.
+// Experts' form (MXFP4).  Every expert's rows in tiles of 128, K in steps of 128; one record per (expert, row tile, step), steps of a
+// tile contiguous:  | codes 8192 | scale atom |      8704 B
+//   codes: row r, byte b of its 64 at (r/8)*512 + (b/16)*128 + (r%8)*16 + b%16; the atom has four scales of 32 K
+// Rows are padded to 128 and K to 128 with zeros: a padded row of a gate is a zero of what follows.
 #pragma once
 #include <stddef.h>
 #include <stdint.h>
@@ -28,7 +26,7 @@ constexpr int KREC = 256;                  // K of a record (linear form)
 constexpr int KSTEP = 128;                 // K of a step (experts' form)
 constexpr uint32_t ATOM = 512;
 constexpr uint32_t CODES = 16384;          // code bytes of a record
-constexpr uint32_t ECODES = 8192;          // code bytes of an expert's tile and step
+constexpr uint32_t ECODES = 8192, ERECORD = ECODES + ATOM;   // of an expert's tile and step
 
 __host__ __device__ constexpr uint32_t atoms(int fmt) { return fmt == SDQ_FMT_NVFP4 ? 4u : 2u; }
 __host__ __device__ constexpr uint32_t record(int fmt) { return CODES + atoms(fmt) * ATOM; }
@@ -36,7 +34,7 @@ __host__ __device__ inline uint32_t atom_off(uint32_t row, uint32_t s) { return 
 
 struct Dims {
   int64_t tiles, kblocks;                  // row tiles (of one expert), records or steps along K
-  size_t off1, off2, total;
+  size_t factors, total;                   // offset of the row factors
 };
 inline Dims dims(int64_t E, int64_t R, int64_t K, int fmt) {
   Dims d;
@@ -44,12 +42,11 @@ inline Dims dims(int64_t E, int64_t R, int64_t K, int fmt) {
   d.tiles = (R + ROWS - 1) / ROWS;
   if (E == 0) {
     d.kblocks = (K + KREC - 1) / KREC;
-    d.off1 = d.off2 = al((size_t)d.tiles * d.kblocks * record(fmt));
-    d.total = d.off2 + (fmt == SDQ_FMT_NVFP4 ? al((size_t)d.tiles * ROWS * 4) : 0);
+    d.factors = al((size_t)d.tiles * d.kblocks * record(fmt));
+    d.total = d.factors + (fmt == SDQ_FMT_NVFP4 ? al((size_t)d.tiles * ROWS * 4) : 0);
   } else {
     d.kblocks = (K + KSTEP - 1) / KSTEP;
-    d.off1 = al((size_t)E * d.tiles * d.kblocks * ECODES);
-    d.off2 = d.total = d.off1 + al((size_t)E * d.tiles * d.kblocks * ATOM);
+    d.factors = d.total = al((size_t)E * d.tiles * d.kblocks * ERECORD);
   }
   return d;
 }
@@ -65,7 +62,7 @@ inline bool fmt_ok(int32_t fmt) { return fmt == SDQ_FMT_MXFP4 || fmt == SDQ_FMT_
 inline bool desc_ok(const sdq_mx4_t* q) {
   if (!q || !q->dev || !fmt_ok(q->fmt) || !size_ok(q->E, q->R, q->K) || (q->E && q->fmt != SDQ_FMT_MXFP4)) return false;
   const Dims d = dims(q->E, q->R, q->K, q->fmt);
-  return q->bytes >= d.total && q->off[0] == 0 && q->off[1] == d.off1 && q->off[2] == d.off2 && ((uintptr_t)q->dev & 255) == 0;
+  return q->bytes >= d.total && q->factors == d.factors && ((uintptr_t)q->dev & 255) == 0;
 }
 
 }  // namespace mx4

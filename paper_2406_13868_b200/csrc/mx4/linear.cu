@@ -513,7 +513,7 @@ extern "C" sdq_status_t sdq_mx4_linear(const sdq_mx4_t* Xq, const sdq_mx4_t* Wq,
   p.flags = device_flags();
   if (!d || !p.flags) return SDQ_ERR_CUDA;
   p.x = (const uint8_t*)Xq->dev; p.w = (const uint8_t*)Wq->dev;
-  p.fx = reinterpret_cast<const float*>(p.x + dx.off2); p.fw = reinterpret_cast<const float*>(p.w + dw.off2);
+  p.fx = reinterpret_cast<const float*>(p.x + dx.factors); p.fw = reinterpret_cast<const float*>(p.w + dw.factors);
   p.bias = bias; p.Y = Y; p.M = Xq->R; p.N = Wq->R; p.ldy = ldy;
   p.kb = (int32_t)dx.kblocks; p.m_tiles = (int32_t)dx.tiles; p.n_tiles = (int32_t)dw.tiles;
   auto go = [&](auto fmt) -> sdq_status_t {

@@ -184,15 +184,15 @@ __device__ __forceinline__ uint4 encode_nv(float (&v)[32], float down, uint32_t&
 
 // ---- where a unit lies -------------------------------------------------------------------------------------------------
 // `g`: 8-row group (linear: of the matrix; experts: of all padded rows), `u`: 128-K unit
-struct Unit { uint8_t* codes; uint8_t* scales; };        // of this lane: 16 B (linear) or two times 8 B 64 apart (experts); the row's word of atom 0
+struct Unit { uint8_t* codes; uint8_t* scales; };        // of this lane: 16 B; the row's word of the unit's first atom
 template <bool EXPERTS, int FMT>
-__device__ __forceinline__ Unit unit_at(uint8_t* buf, size_t off1, int64_t g, int64_t u, int64_t kblocks, uint32_t lane) {
+__device__ __forceinline__ Unit unit_at(uint8_t* buf, int64_t g, int64_t u, int64_t kblocks, uint32_t lane) {
   Unit x;
   const uint32_t rr = (uint32_t)(g & 15) * 8 + (lane >> 2);
   if constexpr (EXPERTS) {
-    const size_t at = (size_t)((g >> 4) * kblocks + u);
-    x.codes = buf + at * ECODES + (uint32_t)(g & 15) * 512 + (lane & 3) * 128 + (lane >> 2) * 8;
-    x.scales = buf + off1 + at * ATOM + atom_off(rr, 0);
+    uint8_t* rec = buf + (size_t)((g >> 4) * kblocks + u) * ERECORD;
+    x.codes = rec + (uint32_t)(g & 15) * 512 + (lane & 3) * 128 + (lane >> 2) * 16;
+    x.scales = rec + ECODES + atom_off(rr, 0);
   } else {
     uint8_t* rec = buf + (size_t)((g >> 4) * kblocks + (u >> 1)) * record(FMT);
     x.codes = rec + (uint32_t)(g & 15) * 1024 + ((uint32_t)(u & 1) * 4 + (lane & 3)) * 128 + (lane >> 2) * 16;
@@ -200,24 +200,8 @@ __device__ __forceinline__ Unit unit_at(uint8_t* buf, size_t off1, int64_t g, in
   }
   return x;
 }
-template <bool EXPERTS>
-__device__ __forceinline__ void put_codes(const Unit& x, uint4 c) {
-  if constexpr (EXPERTS) {
-    *reinterpret_cast<uint2*>(x.codes) = make_uint2(c.x, c.y);
-    *reinterpret_cast<uint2*>(x.codes + 64) = make_uint2(c.z, c.w);
-  } else {
-    *reinterpret_cast<uint4*>(x.codes) = c;
-  }
-}
-template <bool EXPERTS>
-__device__ __forceinline__ uint4 get_codes(const Unit& x) {
-  if constexpr (EXPERTS) {
-    const uint2 a = *reinterpret_cast<const uint2*>(x.codes), b = *reinterpret_cast<const uint2*>(x.codes + 64);
-    return make_uint4(a.x, a.y, b.x, b.y);
-  } else {
-    return *reinterpret_cast<const uint4*>(x.codes);
-  }
-}
+__device__ __forceinline__ void put_codes(const Unit& x, uint4 c) { *reinterpret_cast<uint4*>(x.codes) = c; }
+__device__ __forceinline__ uint4 get_codes(const Unit& x) { return *reinterpret_cast<const uint4*>(x.codes); }
 // the scales of a row's lanes as words (all lanes of the warp): MXFP4 one byte a lane, NVFP4 two
 template <int FMT>
 __device__ __forceinline__ void put_scales(const Unit& x, uint32_t s, uint32_t lane, bool on) {
@@ -246,7 +230,7 @@ __device__ __forceinline__ int64_t element_row(int64_t g, int64_t R, int64_t til
   return r < R ? e * R + r : -1;
 }
 
-struct Shape { int64_t R, K, ld, tiles, kblocks, units; size_t off1, off2; };     // units: 128-K units along K, padding included
+struct Shape { int64_t R, K, ld, tiles, kblocks, units; size_t factors; };          // units: 128-K units along K, padding included
 
 // ---- MXFP4 --------------------------------------------------------------------------------------------------------------
 template <int DT, bool EXPERTS, bool VEC>
@@ -263,9 +247,9 @@ mx4_quantize_kernel(const typename Elem<DT>::type* __restrict__ X, Shape s, int 
     load_unit<DT, VEC>(v, r < 0 ? nullptr : X + r * s.ld, u * UNIT_K, s.K, stage + (VEC ? 0 : warp * Stage<DT>::BYTES), lane);
     uint32_t sc;
     const uint4 c = encode_mx<DT>(v, ceil_rule != 0, sc);
-    const Unit x = unit_at<EXPERTS, SDQ_FMT_MXFP4>(buf, s.off1, g, u, s.kblocks, lane);
+    const Unit x = unit_at<EXPERTS, SDQ_FMT_MXFP4>(buf, g, u, s.kblocks, lane);
     const bool on = EXPERTS || r >= 0;
-    if (on) put_codes<EXPERTS>(x, c);
+    if (on) put_codes(x, c);
     put_scales<SDQ_FMT_MXFP4>(x, sc, lane, on);
   }
 }
@@ -303,13 +287,13 @@ nv4_quantize_kernel(const typename Elem<DT>::type* __restrict__ X, Shape s, uint
   for (uint32_t w = 0; w < warps; ++w) a = fmaxf(a, s_max[w][lane >> 2]);
   const int t = nv_row_exp(fminf(a, type_max<DT>()));
   const float down = pow2_neg(t);
-  if (warp == 0 && (lane & 3) == 0 && r >= 0) *reinterpret_cast<float*>(buf + s.off2 + (size_t)r * 4) = __uint_as_float((uint32_t)(t + 127) << 23);
+  if (warp == 0 && (lane & 3) == 0 && r >= 0) *reinterpret_cast<float*>(buf + s.factors + (size_t)r * 4) = __uint_as_float((uint32_t)(t + 127) << 23);
   for (int64_t u = warp; u < s.units; u += ONE ? s.units : (int64_t)warps) {
     if constexpr (!ONE) load_unit<DT, VEC>(v, row, u * UNIT_K, s.K, st, lane);
     uint32_t sc;
     const uint4 c = encode_nv<DT>(v, down, sc);
-    const Unit x = unit_at<false, SDQ_FMT_NVFP4>(buf, 0, g, u, s.kblocks, lane);
-    if (r >= 0) put_codes<false>(x, c);
+    const Unit x = unit_at<false, SDQ_FMT_NVFP4>(buf, g, u, s.kblocks, lane);
+    if (r >= 0) put_codes(x, c);
     put_scales<SDQ_FMT_NVFP4>(x, sc, lane, r >= 0);
   }
 }
@@ -344,13 +328,13 @@ mx4_import_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__
         if (b < nb) sc |= (uint32_t)scales[r * nb + b] << (8 * i);
       }
     }
-    const Unit x = unit_at<EXPERTS, FMT>(buf, s.off1, g, u, s.kblocks, lane);
+    const Unit x = unit_at<EXPERTS, FMT>(buf, g, u, s.kblocks, lane);
     const bool on = EXPERTS || r >= 0;
-    if (on) put_codes<EXPERTS>(x, make_uint4(w[0], w[1], w[2], w[3]));
+    if (on) put_codes(x, make_uint4(w[0], w[1], w[2], w[3]));
     put_scales<FMT>(x, sc, lane, on);
   }
   if (FMT == SDQ_FMT_NVFP4 && blockIdx.y == 0 && warp == 0 && (lane & 3) == 0 && r >= 0)
-    *reinterpret_cast<float*>(buf + s.off2 + (size_t)r * 4) = factor ? factor[r] : 1.0f;
+    *reinterpret_cast<float*>(buf + s.factors + (size_t)r * 4) = factor ? factor[r] : 1.0f;
 }
 template <int FMT, bool EXPERTS>
 __global__ void __launch_bounds__(32 * Q_WARPS)
@@ -364,8 +348,8 @@ mx4_export_kernel(uint8_t* __restrict__ buf, Shape s, uint8_t* __restrict__ code
   if (r < 0) return;
   const int64_t kb = (s.K + 1) / 2, nb = FMT == SDQ_FMT_NVFP4 ? (s.K + 15) / 16 : (s.K + 31) / 32;
   for (int64_t u = (int64_t)blockIdx.y * Q_WARPS + warp; u < s.units; u += (int64_t)gridDim.y * Q_WARPS) {
-    const Unit x = unit_at<EXPERTS, FMT>(buf, s.off1, g, u, s.kblocks, lane);
-    const uint4 c = get_codes<EXPERTS>(x);
+    const Unit x = unit_at<EXPERTS, FMT>(buf, g, u, s.kblocks, lane);
+    const uint4 c = get_codes(x);
     const uint32_t w[4] = {c.x, c.y, c.z, c.w}, sc = get_scales<FMT>(x, lane);
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
@@ -378,7 +362,7 @@ mx4_export_kernel(uint8_t* __restrict__ buf, Shape s, uint8_t* __restrict__ code
       if (b < nb) scales[r * nb + b] = (uint8_t)(sc >> (8 * i));
     }
   }
-  if (FMT == SDQ_FMT_NVFP4 && factor && blockIdx.y == 0 && warp == 0 && (lane & 3) == 0) factor[r] = *reinterpret_cast<const float*>(buf + s.off2 + (size_t)r * 4);
+  if (FMT == SDQ_FMT_NVFP4 && factor && blockIdx.y == 0 && warp == 0 && (lane & 3) == 0) factor[r] = *reinterpret_cast<const float*>(buf + s.factors + (size_t)r * 4);
 }
 
 // ---- dequantization ------------------------------------------------------------------------------------------------------
@@ -407,12 +391,12 @@ mx4_dequantize_kernel(uint8_t* __restrict__ buf, Shape s, typename Elem<DT>::typ
   const int64_t g = blockIdx.x, r = element_row<EXPERTS>(g, s.R, s.tiles, lane);
   uint8_t* st = stage + (VEC ? 0 : warp * Stage<DT>::BYTES);
   float f = 1.0f;
-  if (FMT == SDQ_FMT_NVFP4 && r >= 0) f = *reinterpret_cast<const float*>(buf + s.off2 + (size_t)r * 4);
+  if (FMT == SDQ_FMT_NVFP4 && r >= 0) f = *reinterpret_cast<const float*>(buf + s.factors + (size_t)r * 4);
   for (int64_t u = (int64_t)blockIdx.y * (blockDim.x >> 5) + warp; u < s.units; u += (int64_t)gridDim.y * (blockDim.x >> 5)) {
     float v[32];
     if (r >= 0) {
-      const Unit x = unit_at<EXPERTS, FMT>(buf, s.off1, g, u, s.kblocks, lane);
-      const uint4 c = get_codes<EXPERTS>(x);
+      const Unit x = unit_at<EXPERTS, FMT>(buf, g, u, s.kblocks, lane);
+      const uint4 c = get_codes(x);
       const uint32_t sc = get_scales<FMT>(x, lane);
       values8(c.x, v);
       values8(c.y, v + 8);
@@ -472,7 +456,7 @@ static Shape shape_of(int64_t E, int64_t R, int64_t K, int64_t ld, int fmt) {
   const Dims d = dims(E, R, K, fmt);
   Shape s;
   s.R = R; s.K = K; s.ld = ld; s.tiles = d.tiles; s.kblocks = d.kblocks; s.units = E ? d.kblocks : 2 * d.kblocks;
-  s.off1 = d.off1; s.off2 = d.off2;
+  s.factors = d.factors;
   return s;
 }
 template <typename... P, typename... A>
@@ -499,7 +483,7 @@ static bool vectors_fit(const void* p, int64_t ld, int64_t K, int32_t dtype, boo
 static void describe(sdq_mx4_t* out, void* buf, int64_t E, int64_t R, int64_t K, int fmt) {
   const Dims d = dims(E, R, K, fmt);
   out->dev = buf; out->bytes = d.total; out->E = E; out->R = R; out->K = K; out->fmt = fmt; out->reserved = 0;
-  out->off[0] = 0; out->off[1] = d.off1; out->off[2] = d.off2;
+  out->factors = d.factors;
 }
 template <int DT>
 static sdq_status_t quantize(const void* X, int64_t E, const Shape& s, int fmt, int rule, uint8_t* buf, void* stream) {

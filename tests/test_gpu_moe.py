@@ -109,14 +109,13 @@ def check_moe(m, T, H, I, E, k, dtype, seed=0, ids=None, x=None, out=None, works
             h = gate * torch.sigmoid(gate) * up
             c = float(weights[t, j])
             want[t] += c * (v2[e] @ h)
-            # gate and up: fp32 sums of H exact products (and of the pieces' rests, 2^-22 of the block's largest magnitude an element)
-            a = v1[e].abs() @ (xd[t].abs() + 2.0 ** -21 * xd[t].abs().max()), v3[e].abs() @ (xd[t].abs() + 2.0 ** -21 * xd[t].abs().max())
-            eps = H * 2.0 ** -23 + 2.0 ** -20
+            # six pieces leave at most 2^-17 of the largest magnitude of an element's block of 32 (the pieces' comment in the kernel)
+            block = lambda v, n: torch.nn.functional.pad(v.abs(), (0, -n % 32)).view(-1, 32).amax(1).repeat_interleave(32)[:n]  # noqa: E731
+            # gate and up: fp32 sums of exact products
+            a = [v[e].abs() @ ((H * 2.0 ** -23 + 2.0 ** -21) * xd[t].abs() + 2.0 ** -17 * block(xd[t], H)) for v in (v1, v3)]
             # silu changes by at most 1.1 times its argument's change
-            dh = 1.1 * eps * a[0] * up.abs() + gate.abs() * eps * a[1] + 2.0 ** -21 * h.abs()
-            # h in three pieces: a piece rounds off 2^-4 of what it is given, and 2^-14 of the block's largest magnitude over 256 at the least
-            blocks = torch.nn.functional.pad(h.abs(), (0, -I % 32)).view(-1, 32).amax(1).repeat_interleave(32)[:I]
-            dh = dh + 2.0 ** -12 * h.abs() + 2.0 ** -24 * blocks
+            dh = 1.1 * a[0] * up.abs() + gate.abs() * a[1] + 1.1 * a[0] * a[1] + 2.0 ** -21 * h.abs()
+            dh = dh + 2.0 ** -17 * block(h.abs() + dh, I)
             bound[t] += abs(c) * (v2[e].abs() @ dh + (I * 2.0 ** -23 + 2.0 ** -21) * (v2[e].abs() @ h.abs()))
     got = y.double()
     eps = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -11

@@ -43,7 +43,7 @@ def test_sizes(m):
     assert L.sdq_mx4_size(4096, 4096, 0, ctypes.byref(b)) == 0 and b.value == 32 * 16 * 17408
     assert L.sdq_mx4_size(0, 4, 0, ctypes.byref(b)) == 2 and L.sdq_mx4_size(4, 0, 0, ctypes.byref(b)) == 2 and L.sdq_mx4_size(4, 4, 2, ctypes.byref(b)) == 1
     assert L.sdq_mx4_size(1 << 36, 1 << 30, 0, ctypes.byref(b)) == 2
-    assert L.sdq_mx4_experts_size(3, 130, 200, ctypes.byref(b)) == 0 and b.value == 3 * 2 * 2 * (8192 + 512)
+    assert L.sdq_mx4_experts_size(3, 130, 200, ctypes.byref(b)) == 0 and b.value == 3 * 2 * 2 * 8704
     assert L.sdq_mx4_experts_size(0, 130, 200, ctypes.byref(b)) == 2
 
 
@@ -73,13 +73,8 @@ def _desc(m, E, R, K, fmt, P=1 << 20):
     d, b = m._Mx4(), ctypes.c_size_t()
     assert (m.lib().sdq_mx4_experts_size(E, R, K, ctypes.byref(b)) if E else m.lib().sdq_mx4_size(R, K, fmt, ctypes.byref(b))) == 0
     d.dev, d.bytes, d.E, d.R, d.K, d.fmt = P, b.value, E, R, K, fmt
-    if E:
-        n = -(-R // 128) * -(-K // 128) * E
-        d.off[1] = (n * 8192 + 255) // 256 * 256
-        d.off[2] = d.off[1] + (n * 512 + 255) // 256 * 256
-    else:
-        n = -(-R // 128) * -(-K // 256) * (18432 if fmt else 17408)
-        d.off[1] = d.off[2] = n
+    n = E * -(-R // 128) * -(-K // 128) * 8704 if E else -(-R // 128) * -(-K // 256) * (18432 if fmt else 17408)
+    d.factors = (n + 255) // 256 * 256
     return d
 
 

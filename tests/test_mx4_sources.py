@@ -37,7 +37,7 @@ def test_global_memory_is_read_behind_the_wait_for_the_launch_in_front(bodies):
         if n in ("moe_up_kernel", "moe_down_kernel"):
             continue
         wait = b.index("ptx::griddep_wait()")
-        for what in (r"ptx::bulk_g2s\(", r"__ldg\(", r"\bload_unit<", r"get_codes<", r"put_codes<", r"codes\[r", r"atomicOr\(", r"\bload8<", r"load_tile\(", r"p\.(?:ids|weights|ws)\b"):
+        for what in (r"ptx::bulk_g2s\(", r"__ldg\(", r"\bload_unit<", r"get_codes\(", r"put_codes\(", r"codes\[r", r"atomicOr\(", r"\bload8<", r"p\.(?:ids|weights|ws)\b"):
             assert all(x.start() > wait for x in re.finditer(what, b)), (n, what)
 
 
