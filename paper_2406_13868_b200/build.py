@@ -18,7 +18,7 @@ BINDING_SOURCE = "sdq_python.cpp"
 SOURCES = ["sdq_api.cu", "sdq_pack.cu", "sdq_quant_act.cu", "sdq_linear.cu", "sdq_linear_pair.cu", "sdq_linear_group.cu", "sdq_plain.cu", "sdq_calib.cu", "sdq_diag.cu",
            "mx4/quant.cu", "mx4/linear.cu", "mx4/route.cu", "mx4/moe.cu"]
 HEADERS = ["sdq_internal.h", "sdq_layout.h", "sdq_linear.h", "sdq_plain.h", "sdq_ptx.cuh", "sdq_codec.cuh", os.path.join("..", "..", "include", "sdq.h"), os.path.join("..", "..", "include", "sdq_diag.h"),
-           os.path.join("mx4", "layout.h"), os.path.join("..", "..", "include", "sdq_mx4.h")]
+           os.path.join("mx4", "layout.h"), os.path.join("mx4", "pipe.cuh"), os.path.join("..", "..", "include", "sdq_mx4.h")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-shared",
               "-Xcompiler", "-fPIC", "--threads", "0"]
 

@@ -24,6 +24,7 @@
 #include "../sdq_internal.h"
 #include "../sdq_ptx.cuh"
 #include "layout.h"
+#include "pipe.cuh"
 
 namespace sdq {
 namespace mx4 {
@@ -232,9 +233,8 @@ struct MoeBars {
   uint32_t tmem, timed_out;
   Plan plan;
 };
-// copies of the scales and the two MMAs (64 K each) of one step; nothing accumulates in front of the first where `acc` is 0
-__device__ __forceinline__ void step_mma(uint32_t d, uint32_t a, uint32_t b, uint32_t sfa, uint32_t sfb, uint32_t id0, uint32_t id2, uint32_t acc) {
-  const uint64_t da = ptx::smem_desc(a, 128, 512), db = ptx::smem_desc(b, 128, 512);
+// the two MMAs (64 K each) of one step; nothing accumulates in front of the first where `acc` is 0
+__device__ __forceinline__ void step_mma(uint32_t d, uint64_t da, uint64_t db, uint32_t sfa, uint32_t sfb, uint32_t id0, uint32_t id2, uint32_t acc) {
   ptx::mma_mxf4(d, da, db, id0, sfa, sfb, acc);
   ptx::mma_mxf4(d, da + (256 >> 4), db + (256 >> 4), id2, sfa, sfb, 1u);
 }
@@ -299,17 +299,19 @@ moe_up_kernel(const __grid_constant__ MoeParams p)
   bool ok = true;
   if (warp == 0) {
     if (lane == 0) {
-      uint32_t i = 0, s = 0, ph = 1;
+      Slot at(b.full, b.empty, sm, 1);
+      uint32_t left = NSLOT;                      // slots that have not been used yet
       for (int task = cluster; task < tasks && ok; task += clusters) {
         const int u = task / p.tiles_i, tile = task - u * p.tiles_i;
-        size_t at = ((size_t)s_unit[u].expert * p.tiles_i + tile) * p.off.sh + k0;
-        for (int k = 0; k < steps; ++k, ++i, ++at) {
-          if (i >= NSLOT && !(ok = ptx::mbar_wait(&b.empty[s], ph))) break;
-          uint8_t* st = sm + (size_t)s * SLOT;
-          ptx::mbar_expect_tx(&b.full[s], 2 * ERECORD);
-          ptx::bulk_g2s(st, p.w1 + at * ERECORD, ERECORD, &b.full[s]);
-          ptx::bulk_g2s(st + ERECORD, p.w3 + at * ERECORD, ERECORD, &b.full[s]);
-          if (++s == NSLOT) { s = 0; ph ^= 1u; }
+        const size_t rec = (((size_t)s_unit[u].expert * p.tiles_i + tile) * p.off.sh + k0) * ERECORD;
+        const uint8_t *w1 = p.w1 + rec, *w3 = p.w3 + rec;
+        for (int k = 0; k < steps; ++k, w1 += ERECORD, w3 += ERECORD) {
+          if (left) --left;
+          else if (!(ok = wait32(at.empty, at.ph))) break;
+          expect32(at.full, 2 * ERECORD);
+          copy32(at.at, w1, ERECORD, at.full);
+          copy32(at.at + ERECORD, w3, ERECORD, at.full);
+          at.next(NSLOT, SLOT);
         }
       }
       if (!ok) atomicOr(&p.flags[FLAG_TIMEOUT], 1u);
@@ -322,19 +324,21 @@ moe_up_kernel(const __grid_constant__ MoeParams p)
   } else if (warp == 2) {
     ptx::griddep_wait();                          // X in pieces
     if (lane == 0) {
-      uint32_t i = 0, s = 0, ph = 1;
+      Slot at(b.full, b.empty, sm, 1);
+      uint32_t left = NSLOT;
       for (int task = cluster; task < tasks && ok; task += clusters) {
         const int u = task / p.tiles_i;
         const MoeUnit un = s_unit[u];
         const uint32_t bytes = (uint32_t)(PIECES * un.n + 7) / 8 * GROUP;
-        const uint8_t *x = p.ws + p.off.xp + ((size_t)k0 * p.off.groups + un.group) * GROUP, *sf = p.ws + p.off.xs + ((size_t)u * p.off.sh + k0) * ATOM;
-        for (int k = 0; k < steps; ++k, ++i, x += (size_t)p.off.groups * GROUP, sf += ATOM) {
-          if (i >= NSLOT && !(ok = ptx::mbar_wait(&b.empty[s], ph))) break;
-          uint8_t* st = sm + (size_t)s * SLOT;
-          ptx::mbar_expect_tx(&b.full[s], bytes + ATOM);
-          ptx::bulk_g2s(st + SL_B, x, bytes, &b.full[s]);
-          ptx::bulk_g2s(st + SL_SFB, sf, ATOM, &b.full[s]);
-          if (++s == NSLOT) { s = 0; ph ^= 1u; }
+        const size_t stride = (size_t)p.off.groups * GROUP;
+        const uint8_t *x = p.ws + p.off.xp + (size_t)k0 * stride + (size_t)un.group * GROUP, *sf = p.ws + p.off.xs + ((size_t)u * p.off.sh + k0) * ATOM;
+        for (int k = 0; k < steps; ++k, x += stride, sf += ATOM) {
+          if (left) --left;
+          else if (!(ok = wait32(at.empty, at.ph))) break;
+          expect32(at.full, bytes + ATOM);
+          copy32(at.at + SL_B, x, bytes, at.full);
+          copy32(at.at + SL_SFB, sf, ATOM, at.full);
+          at.next(NSLOT, SLOT);
         }
       }
       if (!ok) atomicOr(&p.flags[FLAG_TIMEOUT], 1u);
@@ -342,23 +346,28 @@ moe_up_kernel(const __grid_constant__ MoeParams p)
     __syncwarp();
   } else if (warp == 1) {
     if (lane == 0) {
-      uint32_t i = 0, t = 0, s = 0, ph = 0;
+      Slot at(b.full, b.empty, sm, 0);
+      uint32_t t = 0, sf = sets;
+      const uint64_t a0 = ptx::smem_desc(at.at, 128, 512), b0 = a0 + (SL_B >> 4), c0 = ptx::smem_desc(at.at, 0, 128), cb0 = c0 + (SL_SFB >> 4);
+      uint64_t off = 0;
       for (int task = cluster; task < tasks && ok; task += clusters, ++t) {
         const uint32_t N = (uint32_t)(PIECES * s_unit[task / p.tiles_i].n + 15) / 16 * 16, buf = bufs == 2 ? t & 1u : 0u, use = bufs == 2 ? t >> 1 : t;
         const uint32_t acc = tmem + buf * 2 * COLS;
         const uint32_t id0 = ptx::idesc_block_scaled(128, N, 1, false, 0, 0), id2 = ptx::idesc_block_scaled(128, N, 1, false, 2, 2);
         if (use > 0 && !(ok = ptx::mbar_wait(&b.acc_empty[buf], (use - 1) & 1u))) break;
-        for (int k = 0; k < steps; ++k, ++i) {
-          if (!(ok = ptx::mbar_wait(&b.full[s], ph))) break;
+        for (int k = 0; k < steps; ++k) {
+          if (!(ok = wait32(at.full, at.ph))) break;
           ptx::tc_fence_after();
-          const uint32_t st = ptx::smem_u32(sm) + s * SLOT, sf = sets + (i & 1u) * 12u;
-          ptx::tc_cp_32x128b_warpx4(sf, ptx::smem_desc(st + ECODES, 0, 128));
-          ptx::tc_cp_32x128b_warpx4(sf + 4, ptx::smem_desc(st + ERECORD + ECODES, 0, 128));
-          ptx::tc_cp_32x128b_warpx4(sf + 8, ptx::smem_desc(st + SL_SFB, 0, 128));
-          step_mma(acc, st, st + SL_B, sf, sf + 8, id0, id2, k ? 1u : 0u);
-          step_mma(acc + COLS, st + ERECORD, st + SL_B, sf + 4, sf + 8, id0, id2, k ? 1u : 0u);
-          ptx::tc_commit(&b.empty[s]);
-          if (++s == NSLOT) { s = 0; ph ^= 1u; }
+          ptx::tc_cp_32x128b_warpx4(sf, c0 + off + (ECODES >> 4));
+          ptx::tc_cp_32x128b_warpx4(sf + 4, c0 + off + ((ERECORD + ECODES) >> 4));
+          ptx::tc_cp_32x128b_warpx4(sf + 8, cb0 + off);
+          step_mma(acc, a0 + off, b0 + off, sf, sf + 8, id0, id2, k ? 1u : 0u);
+          step_mma(acc + COLS, a0 + off + (ERECORD >> 4), b0 + off, sf + 4, sf + 8, id0, id2, k ? 1u : 0u);
+          commit32(at.empty);
+          sf = sets + (sets + 12u - sf);          // (the other set)
+          off += SLOT >> 4;
+          at.next(NSLOT, SLOT);
+          if (at.s == 0) off = 0;
         }
         if (ok) ptx::tc_commit(&b.acc_full[buf]);
       }
@@ -492,22 +501,23 @@ moe_down_kernel(const __grid_constant__ MoeParams p)
   ptx::tc_fence_after();
   const uint32_t COLS = (uint32_t)(PIECES * plan.most + 15) / 16 * 16;
   const uint32_t SLOT = SL_B + COLS * 64u + ATOM, NSLOT = min((uint32_t)p.ring_bytes / SLOT, (uint32_t)MOE_MAX_SLOTS), SL_SFB = SL_B + COLS * 64u;
-  const uint32_t tmem = b.tmem, sets = tmem + 2 * COLS;
+  const uint32_t tmem = b.tmem, bufs = 2 * COLS + 16 <= (uint32_t)p.tmem_cols ? 2u : 1u, sets = tmem + bufs * COLS;
   const int SI = p.off.si, total = plan.units * SI;                       // steps of a unit, of the tile
   const int g0 = (int)((int64_t)rank * total / ks), g1 = (int)((int64_t)(rank + 1) * total / ks);
   bool ok = true;
   if (warp == 0) {
     if (lane == 0) {
-      uint32_t i = 0, s = 0, ph = 1;
+      Slot at(b.full, b.empty, sm, 1);
+      uint32_t left = NSLOT;
       for (int g = g0; g < g1 && ok;) {
         const int u = g / SI, end = min(g1, (u + 1) * SI);
-        size_t at = ((size_t)s_unit[u].expert * p.tiles_h + tile) * SI + (g - u * SI);
-        for (; g < end; ++g, ++i, ++at) {
-          if (i >= NSLOT && !(ok = ptx::mbar_wait(&b.empty[s], ph))) break;
-          uint8_t* st = sm + (size_t)s * SLOT;
-          ptx::mbar_expect_tx(&b.full[s], ERECORD);
-          ptx::bulk_g2s(st, p.w2 + at * ERECORD, ERECORD, &b.full[s]);
-          if (++s == NSLOT) { s = 0; ph ^= 1u; }
+        const uint8_t* w2 = p.w2 + (((size_t)s_unit[u].expert * p.tiles_h + tile) * SI + (g - u * SI)) * ERECORD;
+        for (; g < end; ++g, w2 += ERECORD) {
+          if (left) --left;
+          else if (!(ok = wait32(at.empty, at.ph))) break;
+          expect32(at.full, ERECORD);
+          copy32(at.at, w2, ERECORD, at.full);
+          at.next(NSLOT, SLOT);
         }
       }
       if (!ok) atomicOr(&p.flags[FLAG_TIMEOUT], 1u);
@@ -520,19 +530,21 @@ moe_down_kernel(const __grid_constant__ MoeParams p)
   } else if (warp == 2) {
     ptx::griddep_wait();                          // h
     if (lane == 0) {
-      uint32_t i = 0, s = 0, ph = 1;
+      Slot at(b.full, b.empty, sm, 1);
+      uint32_t left = NSLOT;
       for (int g = g0; g < g1 && ok;) {
         const int u = g / SI, end = min(g1, (u + 1) * SI), k = g - u * SI;
         const MoeUnit un = s_unit[u];
         const uint32_t bytes = (uint32_t)(PIECES * un.n + 7) / 8 * GROUP;
-        const uint8_t *h = p.ws + p.off.hp + ((size_t)k * p.off.groups + un.group) * GROUP, *sf = p.ws + p.off.hs + ((size_t)u * SI + k) * ATOM;
-        for (; g < end; ++g, ++i, h += (size_t)p.off.groups * GROUP, sf += ATOM) {
-          if (i >= NSLOT && !(ok = ptx::mbar_wait(&b.empty[s], ph))) break;
-          uint8_t* st = sm + (size_t)s * SLOT;
-          ptx::mbar_expect_tx(&b.full[s], bytes + ATOM);
-          ptx::bulk_g2s(st + SL_B, h, bytes, &b.full[s]);
-          ptx::bulk_g2s(st + SL_SFB, sf, ATOM, &b.full[s]);
-          if (++s == NSLOT) { s = 0; ph ^= 1u; }
+        const size_t stride = (size_t)p.off.groups * GROUP;
+        const uint8_t *h = p.ws + p.off.hp + (size_t)k * stride + (size_t)un.group * GROUP, *sf = p.ws + p.off.hs + ((size_t)u * SI + k) * ATOM;
+        for (; g < end; ++g, h += stride, sf += ATOM) {
+          if (left) --left;
+          else if (!(ok = wait32(at.empty, at.ph))) break;
+          expect32(at.full, bytes + ATOM);
+          copy32(at.at + SL_B, h, bytes, at.full);
+          copy32(at.at + SL_SFB, sf, ATOM, at.full);
+          at.next(NSLOT, SLOT);
         }
       }
       if (!ok) atomicOr(&p.flags[FLAG_TIMEOUT], 1u);
@@ -540,23 +552,28 @@ moe_down_kernel(const __grid_constant__ MoeParams p)
     __syncwarp();
   } else if (warp == 1) {
     if (lane == 0) {
-      uint32_t seg = 0, i = 0, s = 0, ph = 0;
+      Slot at(b.full, b.empty, sm, 0);
+      uint32_t seg = 0, sf = sets;
+      const uint64_t a0 = ptx::smem_desc(at.at, 128, 512), b0 = a0 + (SL_B >> 4), ca0 = ptx::smem_desc(at.at + ECODES, 0, 128), cb0 = ptx::smem_desc(at.at + SL_SFB, 0, 128);
+      uint64_t off = 0;
       for (int g = g0; g < g1 && ok; ++seg) {
         const int u = g / SI, end = min(g1, (u + 1) * SI);
-        const uint32_t N = (uint32_t)(PIECES * s_unit[u].n + 15) / 16 * 16, acc = tmem + (seg & 1u) * COLS;
+        const uint32_t N = (uint32_t)(PIECES * s_unit[u].n + 15) / 16 * 16, buf = bufs == 2 ? seg & 1u : 0u, use = bufs == 2 ? seg >> 1 : seg, acc = tmem + buf * COLS;
         const uint32_t id0 = ptx::idesc_block_scaled(128, N, 1, false, 0, 0), id2 = ptx::idesc_block_scaled(128, N, 1, false, 2, 2);
-        if (seg > 1 && !(ok = ptx::mbar_wait(&b.acc_empty[seg & 1u], ((seg >> 1) - 1) & 1u))) break;
-        for (const int first = g; g < end; ++g, ++i) {
-          if (!(ok = ptx::mbar_wait(&b.full[s], ph))) break;
+        if (use > 0 && !(ok = ptx::mbar_wait(&b.acc_empty[buf], (use - 1) & 1u))) break;
+        for (uint32_t more = 0; g < end; ++g, more = 1) {
+          if (!(ok = wait32(at.full, at.ph))) break;
           ptx::tc_fence_after();
-          const uint32_t st = ptx::smem_u32(sm) + s * SLOT, sf = sets + (i & 1u) * 8u;
-          ptx::tc_cp_32x128b_warpx4(sf, ptx::smem_desc(st + ECODES, 0, 128));
-          ptx::tc_cp_32x128b_warpx4(sf + 4, ptx::smem_desc(st + SL_SFB, 0, 128));
-          step_mma(acc, st, st + SL_B, sf, sf + 4, id0, id2, g > first ? 1u : 0u);
-          ptx::tc_commit(&b.empty[s]);
-          if (++s == NSLOT) { s = 0; ph ^= 1u; }
+          ptx::tc_cp_32x128b_warpx4(sf, ca0 + off);
+          ptx::tc_cp_32x128b_warpx4(sf + 4, cb0 + off);
+          step_mma(acc, a0 + off, b0 + off, sf, sf + 4, id0, id2, more);
+          commit32(at.empty);
+          sf = sets + (sets + 8u - sf);
+          off += SLOT >> 4;
+          at.next(NSLOT, SLOT);
+          if (at.s == 0) off = 0;
         }
-        if (ok) ptx::tc_commit(&b.acc_full[seg & 1u]);
+        if (ok) ptx::tc_commit(&b.acc_full[buf]);
       }
       if (!ok) atomicOr(&p.flags[FLAG_TIMEOUT], 1u);
     }
@@ -575,13 +592,14 @@ moe_down_kernel(const __grid_constant__ MoeParams p)
       const int u = g / SI;
       g = min(g1, (u + 1) * SI);
       const MoeUnit un = s_unit[u];
-      if (et == 0 && !(ok = ptx::mbar_wait(&b.acc_full[seg & 1u], (seg >> 1) & 1u))) *timed_out = 1u;
+      const uint32_t buf = bufs == 2 ? seg & 1u : 0u, use = bufs == 2 ? seg >> 1 : seg;
+      if (et == 0 && !(ok = ptx::mbar_wait(&b.acc_full[buf], use & 1u))) *timed_out = 1u;
       ptx::named_bar_sync(1, 128);
       if (*timed_out) break;
       ptx::tc_fence_after();
       for (int t0 = 0; t0 < un.n; t0 += CHUNK) {
         float v[CHUNK];
-        load_tokens(tmem + ((q * 32u) << 16) + (seg & 1u) * COLS + (uint32_t)(PIECES * t0), v);
+        load_tokens(tmem + ((q * 32u) << 16) + buf * COLS + (uint32_t)(PIECES * t0), v);
 #pragma unroll
         for (int j = 0; j < CHUNK; ++j)
           if (t0 + j < un.n) {
@@ -591,7 +609,7 @@ moe_down_kernel(const __grid_constant__ MoeParams p)
       }
       ptx::tc_fence_before();
       __syncwarp();
-      if (lane == 0) ptx::mbar_arrive(&b.acc_empty[seg & 1u]);
+      if (lane == 0) ptx::mbar_arrive(&b.acc_empty[buf]);
     }
     if (et == 0 && !ok) atomicOr(&p.flags[FLAG_TIMEOUT], 1u);
     __syncwarp();
@@ -681,9 +699,12 @@ static sdq_status_t moe(MoeParams p, DeviceInfo* d, void* stream) {
     if (st != SDQ_OK) return st;
   }
   {
+    // two CTAs an SM, twice as many as SMs where there is work for them: an SM's two MMA issuers hide each other's trips, and the SMs that
+    // have one CTA get the more of the memory's bandwidth (128 CTAs, one an SM: ..)
+    p.tmem_cols = 256;
     int ks = 1;
-    while (ks < 8 && 2 * ks * p.tiles_h <= d->sm_count) ks *= 2;
-    const uint32_t behind = (uint32_t)p.T * 512u + (uint32_t)pairs * 8u + (uint32_t)p.max_units * (uint32_t)sizeof(MoeUnit);
+    while (ks < 8 && 2 * ks * p.tiles_h <= 2 * d->sm_count && 2 * ks <= p.max_units * p.off.si) ks *= 2;
+    const uint32_t room = SMEM_MAX / 2 - 1024 - 1024 - 128, behind = (uint32_t)p.T * 512u + (uint32_t)pairs * 8u + (uint32_t)p.max_units * (uint32_t)sizeof(MoeUnit);
     p.ring_bytes = (int32_t)((room - behind) / 128 * 128);
     Launch l((unsigned)(p.tiles_h * ks), MOE_THREADS, (unsigned)ks, (size_t)p.ring_bytes + behind + 128, stream);
     return launch_status(cudaLaunchKernelEx(&l.lc, down, p));

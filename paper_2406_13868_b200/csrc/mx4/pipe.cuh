@@ -1,0 +1,38 @@
+// The ring's operations on 32-bit shared-memory addresses.  One thread fills a ring and one thread empties it, and a trip of either loop has to be
+// shorter than what it moves takes: a thread alone issues an instruction every few clocks, so addresses and descriptors are kept and
+// stepped instead of being worked out in every trip.
+#pragma once
+#include "../sdq_ptx.cuh"
+
+namespace sdq {
+namespace mx4 {
+
+__device__ __forceinline__ bool wait32(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  for (uint32_t i = 0; !ok && i < (1u << 22); ++i)
+    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ void expect32(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy32(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void commit32(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+// position in a ring of `n` slots: barriers 8 bytes apart, data `size` bytes apart; `ph` flips with every lap
+struct Slot {
+  uint32_t s, ph, full, empty, at;
+  __device__ __forceinline__ Slot(const uint64_t* full0, const uint64_t* empty0, const void* data, uint32_t phase)
+      : s(0), ph(phase), full(ptx::smem_u32(full0)), empty(ptx::smem_u32(empty0)), at(ptx::smem_u32(data)) {}
+  __device__ __forceinline__ void next(uint32_t n, uint32_t size) {
+    ++s; full += 8; empty += 8; at += size;
+    if (s == n) { s = 0; ph ^= 1u; full -= 8 * n; empty -= 8 * n; at -= size * n; }
+  }
+};
+
+}  // namespace mx4
+}  // namespace sdq
