@@ -1,7 +1,7 @@
 // Plain microscaled 4-bit matrices: quantizers, importer, exporter, dequantizer (formats: include/sdq_mx4.h, layouts: layout.h).
 //
-// All of them work in units of 8 rows x 128 K, one a warp: lane l has row l / 4, elements 32 (l % 4) .. + 31, so that the codes of a unit are 512
-// contiguous bytes and a row's four MXFP4 scales (eight NVFP4 scales) one (two) words of a scale atom.
+// All of them work in units of 8 rows x 128 K, one a warp, as two halves of 64 K: lane l has row l / 4, elements 16 (l % 4) .. + 15 of a half.  An
+// access of a lane is 32 bytes (of a 16-bit type) and four lanes have a line of 128; a store of codes writes whole core matrices.
 //
 // Bound by DRAM traffic: 2 to 4 bytes an element on one side, 0.53 or 0.56 on the other.
 #include <cuda_fp16.h>
@@ -34,57 +34,143 @@ template <int DT> __device__ __forceinline__ typename Elem<DT>::type from_float(
 
 constexpr int Q_WARPS = 8;
 constexpr int UNIT_K = 128;
-// staging of rows that no vector access fits: one unit, rows 16 bytes apart from their neighbours' banks
-template <int DT> struct Stage { static constexpr uint32_t PITCH = UNIT_K * sizeof(typename Elem<DT>::type) + 16, BYTES = 8 * PITCH; };
 
-// this lane's 32 elements of the unit whose first row's unit starts at column k0; `row`: this lane's row (nullptr: none), zeros behind K
-template <int DT, bool VEC>
-__device__ __forceinline__ void load_unit(float (&v)[32], const typename Elem<DT>::type* row, int64_t k0, int64_t K, uint8_t* stage, uint32_t lane) {
-  using T = typename Elem<DT>::type;
-  constexpr int PER = 16 / sizeof(T);                      // elements of a 16-byte load
-  uint4 raw[32 / PER];
-  if constexpr (VEC) {
-    const int64_t k = k0 + 32 * (lane & 3);
+// ---- rows in memory ------------------------------------------------------------------------------------------------------
+// Rows whose elements lie on 32-byte boundaries are loaded and stored 32 bytes a lane (VEC).  Any others go through the 16-byte granules
+// around them: a load takes the granules that overlap its bytes and shifts them into place, a store is turned in shared memory.
+// Single elements are only touched where a granule is not whole inside the matrix.
+struct Bounds { uintptr_t lo, hi; };                        // first byte of the matrix, and the one behind its last
+
+__device__ __forceinline__ void ld32(uint32_t (&w)[8], const void* p) {
+  asm volatile("ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
+}
+__device__ __forceinline__ void st32(void* p, const uint32_t (&w)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+               : "memory");
+}
+// 32 bytes at `p`, of which the first `valid` belong to the row (zeros behind them)
+template <int ES>
+__device__ __forceinline__ void ld32_any(uint32_t (&w)[8], const uint8_t* p, int valid, const Bounds& m) {
+  const uintptr_t at = (uintptr_t)p, g = at & ~(uintptr_t)15;
+  const uint32_t o = (uint32_t)(at & 15);
+  uint32_t x[12];
 #pragma unroll
-    for (int i = 0; i < 32 / PER; ++i) {
-      raw[i] = make_uint4(0, 0, 0, 0);
-      if (row && k + i * PER < K) raw[i] = *reinterpret_cast<const uint4*>(row + k + i * PER);
-    }
-  } else {
-    // rows of any alignment: consecutive lanes take consecutive elements, and the unit is turned in shared memory
+  for (int i = 0; i < 3; ++i) {
+    uint4 v = make_uint4(0, 0, 0, 0);
+    const uintptr_t q = g + 16 * i;
+    if (valid > 0 && q < at + (uintptr_t)valid) {              // (its first byte in front of the row's end; its last one behind `at`)
+      if (q >= m.lo && q + 16 <= m.hi) {
+        v = *reinterpret_cast<const uint4*>(q);
+      } else {
+        uint32_t e[4] = {0, 0, 0, 0};
 #pragma unroll
-    for (int r = 0; r < 8; ++r) {
-      const T* p = reinterpret_cast<const T*>(__shfl_sync(0xffffffffu, (unsigned long long)(uintptr_t)row, 4 * r));
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int64_t k = k0 + 32 * i + lane;
-        T x = from_float<DT>(0.0f);
-        if (p && k < K) x = p[k];
-        *reinterpret_cast<T*>(stage + r * Stage<DT>::PITCH + (32 * i + lane) * sizeof(T)) = x;
+        for (int j = 0; j < 16 / ES; ++j) {
+          const uintptr_t r = q + ES * j;
+          if (r >= at && r < at + (uintptr_t)valid) {
+            if constexpr (ES == 2) e[j / 2] |= (uint32_t)*reinterpret_cast<const uint16_t*>(r) << (16 * (j & 1));
+            else e[j] = *reinterpret_cast<const uint32_t*>(r);
+          }
+        }
+        v = make_uint4(e[0], e[1], e[2], e[3]);
       }
     }
-    __syncwarp();
-    const uint4* s = reinterpret_cast<const uint4*>(stage + (lane >> 2) * Stage<DT>::PITCH + (lane & 3) * 32 * sizeof(T));
-#pragma unroll
-    for (int i = 0; i < 32 / PER; ++i) raw[i] = s[i];
-    __syncwarp();
+    x[4 * i] = v.x; x[4 * i + 1] = v.y; x[4 * i + 2] = v.z; x[4 * i + 3] = v.w;
   }
+  // down by 8, 4 and 2 bytes
 #pragma unroll
-  for (int i = 0; i < 32 / PER; ++i) {
-    const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+  for (int i = 0; i < 10; ++i) x[i] = o & 8 ? x[i + 2] : x[i];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if constexpr (DT == SDQ_FP32) v[4 * i + j] = __uint_as_float(w[j]);
+  for (int i = 0; i < 9; ++i) x[i] = o & 4 ? x[i + 1] : x[i];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w[i] = ES == 2 && (o & 2) ? __funnelshift_r(x[i], x[i + 1], 16) : x[i];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {                             // what lies behind the row's end
+    if (valid < 4 * i + 4) w[i] = ES == 2 && valid == 4 * i + 2 ? w[i] & 0xFFFFu : 0u;
+  }
+}
+// 16 elements of a row from `p`, `n` of which exist
+template <int DT, bool VEC>
+__device__ __forceinline__ void load16(float (&v)[16], const typename Elem<DT>::type* p, int64_t n, const Bounds& m) {
+  constexpr int ES = sizeof(typename Elem<DT>::type), PER = 32 / ES;      // elements of 32 bytes
+#pragma unroll
+  for (int i = 0; i < 16 / PER; ++i) {
+    uint32_t w[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] = 0;
+    const int64_t left = n - i * PER;
+    if constexpr (VEC) { if (left > 0) ld32(w, p + i * PER); }
+    else ld32_any<ES>(w, reinterpret_cast<const uint8_t*>(p + i * PER), (int)(left < 0 ? 0 : left > PER ? PER : left) * ES, m);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if constexpr (DT == SDQ_FP32) v[8 * i + j] = __uint_as_float(w[j]);
       else if constexpr (DT == SDQ_BF16) {
-        v[8 * i + 2 * j] = __uint_as_float(w[j] << 16);
-        v[8 * i + 2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
+        v[2 * j] = __uint_as_float(w[j] << 16);
+        v[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
       } else {
         const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[j]));
-        v[8 * i + 2 * j] = f.x;
-        v[8 * i + 2 * j + 1] = f.y;
+        v[2 * j] = f.x;
+        v[2 * j + 1] = f.y;
       }
     }
   }
+}
+template <int DT>
+__device__ __forceinline__ void pack16(uint32_t (&w)[16 * sizeof(typename Elem<DT>::type) / 4], const float (&v)[16]) {
+#pragma unroll
+  for (int j = 0; j < (int)(16 * sizeof(typename Elem<DT>::type) / 4); ++j) {
+    if constexpr (DT == SDQ_FP32) w[j] = __float_as_uint(v[j]);
+    else if constexpr (DT == SDQ_BF16) {
+      const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
+      w[j] = *reinterpret_cast<const uint32_t*>(&b);
+    } else {
+      const __half2 b = __floats2half2_rn(v[2 * j], v[2 * j + 1]);
+      w[j] = *reinterpret_cast<const uint32_t*>(&b);
+    }
+  }
+}
+// a warp's unit on its way to rows of any alignment: a row's bytes at the offset in a granule that they have in memory
+template <int DT> struct Stage { static constexpr uint32_t ROW = UNIT_K * sizeof(typename Elem<DT>::type), PITCH = ROW + 48, BYTES = 8 * PITCH; };
+template <int DT>
+__device__ __forceinline__ void stage16(uint8_t* st, uint32_t o, uint32_t k, const uint32_t (&w)[16 * sizeof(typename Elem<DT>::type) / 4]) {
+  constexpr int W = 16 * sizeof(typename Elem<DT>::type) / 4;
+  uint8_t* d = st + o + k * sizeof(typename Elem<DT>::type);
+  if (DT != SDQ_FP32 && (o & 2)) {
+    *reinterpret_cast<uint16_t*>(d) = (uint16_t)w[0];
+#pragma unroll
+    for (int j = 0; j + 1 < W; ++j) *reinterpret_cast<uint32_t*>(d + 2 + 4 * j) = __funnelshift_r(w[j], w[j + 1], 16);
+    *reinterpret_cast<uint16_t*>(d + 4 * W - 2) = (uint16_t)(w[W - 1] >> 16);
+  } else {
+#pragma unroll
+    for (int j = 0; j < W; ++j) *reinterpret_cast<uint32_t*>(d + 4 * j) = w[j];
+  }
+}
+// stores the staged rows: row r's first byte is row[r] (of lane 4 r), `bytes` of each exist
+template <int DT>
+__device__ __forceinline__ void store_staged(const uint8_t* st, typename Elem<DT>::type* row, int bytes, uint32_t lane) {
+  using S = Stage<DT>;
+  constexpr int ES = sizeof(typename Elem<DT>::type), GR = (int)S::ROW / 16 + 1;     // granules a row may touch
+  __syncwarp();
+#pragma unroll 1
+  for (int i = (int)lane; i < (8 * GR + 31) / 32 * 32; i += 32) {
+    const int r = i / GR, g = i - r * GR;
+    const uintptr_t p = (uintptr_t)__shfl_sync(0xffffffffu, (unsigned long long)(uintptr_t)row, 4 * (r & 7));
+    if (r >= 8 || !p) continue;
+    const int o = (int)(p & 15), lo = 16 * g, hi = lo + 16;                            // the granule, counted from the first one's start
+    const uint8_t* s = st + r * S::PITCH + lo;
+    uint8_t* d = reinterpret_cast<uint8_t*>(p - o) + lo;
+    if (lo >= o && hi <= o + bytes) {
+      *reinterpret_cast<uint4*>(d) = *reinterpret_cast<const uint4*>(s);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 16; j += ES)
+        if (lo + j >= o && lo + j < o + bytes) {
+          if constexpr (ES == 2) *reinterpret_cast<uint16_t*>(d + j) = *reinterpret_cast<const uint16_t*>(s + j);
+          else *reinterpret_cast<uint32_t*>(d + j) = *reinterpret_cast<const uint32_t*>(s + j);
+        }
+    }
+  }
+  __syncwarp();
 }
 // larger of a and |x|; a NaN stays
 __device__ __forceinline__ float max_abs(float a, float x) {
@@ -92,18 +178,21 @@ __device__ __forceinline__ float max_abs(float a, float x) {
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(fabsf(x)));
   return r;
 }
-// largest magnitude of N elements; where it is an infinity, the elements are limited to the type's largest number first
-template <int DT, int FIRST, int N>
-__device__ __forceinline__ float block_max(float (&v)[32]) {
+// largest magnitude of 16 elements (a NaN stays)
+__device__ __forceinline__ float max16(const float (&v)[16]) {
   float a = 0.0f;
 #pragma unroll
-  for (int i = FIRST; i < FIRST + N; ++i) a = max_abs(a, v[i]);
+  for (int i = 0; i < 16; ++i) a = max_abs(a, v[i]);
+  return a;
+}
+// infinities as the type's largest number; `a`: the block's largest magnitude
+template <int DT>
+__device__ __forceinline__ void saturate(float (&v)[16], float& a) {
   if (a == INFINITY) {
 #pragma unroll
-    for (int i = FIRST; i < FIRST + N; ++i) v[i] = fminf(fmaxf(v[i], -type_max<DT>()), type_max<DT>());
+    for (int i = 0; i < 16; ++i) v[i] = fminf(fmaxf(v[i], -type_max<DT>()), type_max<DT>());
     a = type_max<DT>();
   }
-  return a;
 }
 
 // ---- quotients ---------------------------------------------------------------------------------------------------------
@@ -135,91 +224,84 @@ __device__ __forceinline__ uint32_t mx_scale_code(float a, bool ceil_rule) {
   return (uint32_t)max((int)(b >> 23) - 2 + ((ceil_rule && (b & 0x7FFFFFu) > 0x400000u) ? 1 : 0), 0);
 }
 
-// codes of 32 elements, 16 bytes
-__device__ __forceinline__ uint4 codes32(const float (&q)[32]) {
-  uint32_t w[4];
+// codes of 16 elements, 8 bytes
+__device__ __forceinline__ uint2 codes16(const float (&q)[16]) {
+  float lo[8], hi[8];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float t[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) t[j] = q[8 * i + j];
-    w[i] = e2m1x8(t);
-  }
-  return make_uint4(w[0], w[1], w[2], w[3]);
+  for (int j = 0; j < 8; ++j) { lo[j] = q[j]; hi[j] = q[8 + j]; }
+  return make_uint2(e2m1x8(lo), e2m1x8(hi));
 }
-// MXFP4: codes and the scale's code
+// MXFP4: 16 elements of a block whose other half the neighbouring lane has
 template <int DT>
-__device__ __forceinline__ uint4 encode_mx(float (&v)[32], bool ceil_rule, uint32_t& scale) {
-  const float a = block_max<DT, 0, 32>(v);
+__device__ __forceinline__ uint2 encode_mx(float (&v)[16], bool ceil_rule, uint32_t& scale) {
+  float a = max16(v);
+  a = max_abs(a, __shfl_xor_sync(0xffffffffu, a, 1));
+  saturate<DT>(v, a);
   const uint32_t c = mx_scale_code(a, ceil_rule);
   const float inv = pow2_inv_e8m0(min(c, 253u));
 #pragma unroll
-  for (int i = 0; i < 32; ++i) v[i] *= inv;
+  for (int i = 0; i < 16; ++i) v[i] *= inv;
   scale = a != a ? 255u : c;
-  return codes32(v);
+  return codes16(v);
 }
-// NVFP4: 16 elements as quotients and their scale's code; `down` = 2^-t
-template <int DT, int FIRST>
-__device__ __forceinline__ uint32_t encode_nv16(float (&v)[32], float down) {
-  const float a = block_max<DT, FIRST, 16>(v);
-  const uint32_t c = a != a ? 127u : nv_scale_code(a * down, a > 0.0f);
-  const float s = e4m3_value(c), r = c ? __frcp_rn(s) : 0.0f;
+// NVFP4: a block; `down` = 2^-t of the row
+template <int DT>
+__device__ __forceinline__ uint2 encode_nv(float (&v)[16], float down, uint32_t& scale) {
+  float a = max16(v);
+  saturate<DT>(v, a);
+  scale = a != a ? 127u : nv_scale_code(a * down, a > 0.0f);
+  const float s = e4m3_value(scale), r = scale ? __frcp_rn(s) : 0.0f;
 #pragma unroll
-  for (int i = FIRST; i < FIRST + 16; ++i) {
+  for (int i = 0; i < 16; ++i) {
     // y / s correctly rounded (Markstein: quotient estimate, its exact remainder, one correction): ties stay ties
     const float y = v[i] * down, q = y * r;
     // (the remainder taken as q s - y, so that a negative zero stays one)
     const float z = fmaf(-fmaf(q, s, -y), r, q);
     v[i] = DT == SDQ_FP32 ? keep_side<21>(z, y, s) : z;
   }
-  return c;
-}
-// codes and the two scales' codes (in the two low bytes)
-template <int DT>
-__device__ __forceinline__ uint4 encode_nv(float (&v)[32], float down, uint32_t& scales) {
-  scales = encode_nv16<DT, 0>(v, down);
-  scales |= encode_nv16<DT, 16>(v, down) << 8;
-  return codes32(v);
+  return codes16(v);
 }
 
 // ---- where a unit lies -------------------------------------------------------------------------------------------------
 // `g`: 8-row group (linear: of the matrix; experts: of all padded rows), `u`: 128-K unit
-struct Unit { uint8_t* codes; uint8_t* scales; };        // of this lane: 16 B; the row's word of the unit's first atom
+struct Unit { uint8_t* codes; uint8_t* scales; };        // of this lane's eight code bytes of the first half (the second's: 256 further on); the row's word of the unit's first atom
 template <bool EXPERTS, int FMT>
 __device__ __forceinline__ Unit unit_at(uint8_t* buf, int64_t g, int64_t u, int64_t kblocks, uint32_t lane) {
   Unit x;
   const uint32_t rr = (uint32_t)(g & 15) * 8 + (lane >> 2);
   if constexpr (EXPERTS) {
     uint8_t* rec = buf + (size_t)((g >> 4) * kblocks + u) * ERECORD;
-    x.codes = rec + (uint32_t)(g & 15) * 512 + (lane & 3) * 128 + (lane >> 2) * 16;
+    x.codes = rec + (uint32_t)(g & 15) * 512 + ((lane >> 1) & 1) * 128 + (lane >> 2) * 16 + (lane & 1) * 8;
     x.scales = rec + ECODES + atom_off(rr, 0);
   } else {
     uint8_t* rec = buf + (size_t)((g >> 4) * kblocks + (u >> 1)) * record(FMT);
-    x.codes = rec + (uint32_t)(g & 15) * 1024 + ((uint32_t)(u & 1) * 4 + (lane & 3)) * 128 + (lane >> 2) * 16;
+    x.codes = rec + (uint32_t)(g & 15) * 1024 + ((uint32_t)(u & 1) * 4 + ((lane >> 1) & 1)) * 128 + (lane >> 2) * 16 + (lane & 1) * 8;
     x.scales = rec + CODES + (uint32_t)(u & 1) * (atoms(FMT) / 2) * ATOM + atom_off(rr, 0);
   }
   return x;
 }
-__device__ __forceinline__ void put_codes(const Unit& x, uint4 c) { *reinterpret_cast<uint4*>(x.codes) = c; }
-__device__ __forceinline__ uint4 get_codes(const Unit& x) { return *reinterpret_cast<const uint4*>(x.codes); }
-// the scales of a row's lanes as words (all lanes of the warp): MXFP4 one byte a lane, NVFP4 two
+__device__ __forceinline__ void put_codes(const Unit& x, int half, uint2 c) { *reinterpret_cast<uint2*>(x.codes + 256 * half) = c; }
+__device__ __forceinline__ uint2 get_codes(const Unit& x, int half) { return *reinterpret_cast<const uint2*>(x.codes + 256 * half); }
+// the scales of a row's lanes as words (all lanes of the warp): MXFP4: two of each half, one word; NVFP4: four of a half, a word each
 template <int FMT>
-__device__ __forceinline__ void put_scales(const Unit& x, uint32_t s, uint32_t lane, bool on) {
+__device__ __forceinline__ void put_scales(const Unit& x, const uint32_t (&s)[2], uint32_t lane, bool on) {
   if constexpr (FMT == SDQ_FMT_MXFP4) {
-    uint32_t w = s << (8 * (lane & 3));
-    w |= __shfl_xor_sync(0xffffffffu, w, 1);
+    uint32_t w = (s[0] | s[1] << 16) << (4 * (lane & 2));             // (both lanes of a pair have its scale)
     w |= __shfl_xor_sync(0xffffffffu, w, 2);
     if (on && (lane & 3) == 0) *reinterpret_cast<uint32_t*>(x.scales) = w;
   } else {
-    uint32_t w = s << (16 * (lane & 1));
-    w |= __shfl_xor_sync(0xffffffffu, w, 1);
-    if (on && (lane & 1) == 0) *reinterpret_cast<uint32_t*>(x.scales + ((lane >> 1) & 1) * ATOM) = w;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      uint32_t w = s[h] << (8 * (lane & 3));
+      w |= __shfl_xor_sync(0xffffffffu, w, 1);
+      w |= __shfl_xor_sync(0xffffffffu, w, 2);
+      if (on && (lane & 3) == (uint32_t)h) *reinterpret_cast<uint32_t*>(x.scales + h * ATOM) = w;
+    }
   }
 }
 template <int FMT>
-__device__ __forceinline__ uint32_t get_scales(const Unit& x, uint32_t lane) {
-  if constexpr (FMT == SDQ_FMT_MXFP4) return x.scales[lane & 3];
-  else return *reinterpret_cast<const uint16_t*>(x.scales + ((lane >> 1) & 1) * ATOM + 2 * (lane & 1));
+__device__ __forceinline__ uint32_t get_scale(const Unit& x, int half, uint32_t lane) {
+  return FMT == SDQ_FMT_MXFP4 ? x.scales[2 * half + ((lane >> 1) & 1)] : x.scales[half * ATOM + (lane & 3)];
 }
 // element row of a lane: linear: row 8 g + l / 4; experts: padded rows are none (-1)
 template <bool EXPERTS>
@@ -230,71 +312,129 @@ __device__ __forceinline__ int64_t element_row(int64_t g, int64_t R, int64_t til
   return r < R ? e * R + r : -1;
 }
 
-struct Shape { int64_t R, K, ld, tiles, kblocks, units; size_t factors; };          // units: 128-K units along K, padding included
+struct Shape { int64_t R, rows, K, ld, tiles, kblocks, units; size_t factors; };          // rows: of all experts; units: 128-K units along K, padding included
+
+template <int DT>
+__device__ __forceinline__ Bounds bounds_of(const typename Elem<DT>::type* X, const Shape& s) {
+  return Bounds{(uintptr_t)X, (uintptr_t)(X + (s.rows - 1) * s.ld + s.K)};
+}
 
 // ---- MXFP4 --------------------------------------------------------------------------------------------------------------
 template <int DT, bool EXPERTS, bool VEC>
 __global__ void __launch_bounds__(32 * Q_WARPS)
 mx4_quantize_kernel(const typename Elem<DT>::type* __restrict__ X, Shape s, int ceil_rule, uint8_t* __restrict__ buf)
 {
-  __shared__ __align__(16) uint8_t stage[VEC ? 16 : Q_WARPS * Stage<DT>::BYTES];
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) ptx::griddep_launch_dependents();
   ptx::griddep_wait();
   const int64_t g = blockIdx.x, r = element_row<EXPERTS>(g, s.R, s.tiles, lane);
+  const Bounds m = bounds_of<DT>(X, s);
   for (int64_t u = (int64_t)blockIdx.y * (blockDim.x >> 5) + warp; u < s.units; u += (int64_t)gridDim.y * (blockDim.x >> 5)) {
-    float v[32];
-    load_unit<DT, VEC>(v, r < 0 ? nullptr : X + r * s.ld, u * UNIT_K, s.K, stage + (VEC ? 0 : warp * Stage<DT>::BYTES), lane);
-    uint32_t sc;
-    const uint4 c = encode_mx<DT>(v, ceil_rule != 0, sc);
+    const int64_t k = u * UNIT_K + 16 * (lane & 3);
+    float v[2][16];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) load16<DT, VEC>(v[h], X + r * s.ld + k + 64 * h, r < 0 ? 0 : s.K - k - 64 * h, m);
     const Unit x = unit_at<EXPERTS, SDQ_FMT_MXFP4>(buf, g, u, s.kblocks, lane);
     const bool on = EXPERTS || r >= 0;
-    if (on) put_codes(x, c);
+    uint32_t sc[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint2 c = encode_mx<DT>(v[h], ceil_rule != 0, sc[h]);
+      if (on) put_codes(x, h, c);
+    }
     put_scales<SDQ_FMT_MXFP4>(x, sc, lane, on);
   }
 }
 
 // ---- NVFP4 --------------------------------------------------------------------------------------------------------------
-// One CTA per 8 rows: the rows' maxima first, then every unit again (from L2, where the first pass has left it) to be encoded.
-// (staging of fp32 rows: eight warps' is what shared memory has without asking for more)
-template <int DT, bool VEC> struct NvWarps { static constexpr int value = !VEC && DT == SDQ_FP32 ? 8 : 16; };
-// ONE: rows of at most one unit a warp, which stays in registers between the two passes.  (As a condition on the second load instead of
-// a form of its own, ptxas 12.9 at -O1 and above lost the upper elements.)
-template <int DT, bool VEC, bool ONE>
-__global__ void __launch_bounds__(32 * NvWarps<DT, VEC>::value)
-nv4_quantize_kernel(const typename Elem<DT>::type* __restrict__ X, Shape s, uint8_t* __restrict__ buf)
-{
-  __shared__ __align__(16) uint8_t stage[VEC ? 16 : NvWarps<DT, VEC>::value * Stage<DT>::BYTES];
-  __shared__ float s_max[16][8];
-  const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-  uint8_t* st = stage + (VEC ? 0 : warp * Stage<DT>::BYTES);
-  if (threadIdx.x == 0) ptx::griddep_launch_dependents();
-  ptx::griddep_wait();
-  const int64_t g = blockIdx.x, r = element_row<false>(g, s.R, s.tiles, lane);
-  const typename Elem<DT>::type* row = r < 0 ? nullptr : X + r * s.ld;
-  float a = 0.0f;
-  float v[32];
-  for (int64_t u = warp; u < s.units; u += ONE ? s.units : (int64_t)warps) {
-    load_unit<DT, VEC>(v, row, u * UNIT_K, s.K, st, lane);
-    // (a NaN's block is marked by its scale; the row's factor goes by the others)
-#pragma unroll
-    for (int i = 0; i < 32; ++i) a = fmaxf(a, fabsf(v[i]));
-  }
+// The CTAs of a cluster share the units of 8 rows, NU a warp, which stay in registers while the rows' maxima are exchanged through
+// distributed shared memory.  Rows too long for that (LONG) are read twice, by one CTA a group, the second time from L2.
+// This CTA's maxima of the eight rows, and where the other CTAs put theirs
+constexpr int NV_CTAS = 8;
+struct NvMax { float warp[Q_WARPS][8], cta[NV_CTAS][8]; };
+__device__ __forceinline__ float max_over_cluster(NvMax& m, float a, uint32_t warp, uint32_t lane, uint32_t warps, uint32_t ctas, uint32_t rank) {
   a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 1));
   a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 2));
-  if ((lane & 3) == 0) s_max[warp][lane >> 2] = a;
+  if ((lane & 3) == 0) m.warp[warp][lane >> 2] = a;
   __syncthreads();
-  for (uint32_t w = 0; w < warps; ++w) a = fmaxf(a, s_max[w][lane >> 2]);
+  if (ctas == 1) {
+    for (uint32_t w = 0; w < warps; ++w) a = fmaxf(a, m.warp[w][lane >> 2]);
+    return a;
+  }
+  ptx::cluster_sync();                       // (every CTA has started, too: its shared memory may be written)
+  if (threadIdx.x < 8 * ctas) {
+    const uint32_t row = threadIdx.x & 7, peer = threadIdx.x >> 3;
+    float t = 0.0f;
+    for (uint32_t w = 0; w < warps; ++w) t = fmaxf(t, m.warp[w][row]);
+    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(ptx::mapa_u32(ptx::smem_u32(&m.cta[rank][row]), peer)), "f"(t) : "memory");
+  }
+  ptx::cluster_sync();
+  for (uint32_t c = 0; c < ctas; ++c) a = fmaxf(a, m.cta[c][lane >> 2]);
+  return a;
+}
+template <int DT, bool VEC, int NU, bool LONG>
+__global__ void __launch_bounds__(32 * Q_WARPS)
+nv4_quantize_kernel(const typename Elem<DT>::type* __restrict__ X, Shape s, uint8_t* __restrict__ buf)
+{
+  __shared__ NvMax mx;
+  const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+  if (threadIdx.x == 0) ptx::griddep_launch_dependents();
+  ptx::griddep_wait();
+  const uint32_t ctas = LONG ? 1u : gridDim.y, rank = LONG ? 0u : blockIdx.y;
+  const int64_t g = blockIdx.x, r = element_row<false>(g, s.R, s.tiles, lane);
+  const Bounds m = bounds_of<DT>(X, s);
+  const typename Elem<DT>::type* row = X + r * s.ld + 16 * (lane & 3);
+  const int64_t have = r < 0 ? 0 : s.K - 16 * (lane & 3);
+  float a = 0.0f, v[NU][2][16];
+  // (a NaN's block is marked by its scale; the row's factor goes by the others)
+  if constexpr (LONG) {
+    for (int64_t u = warp; u < s.units; u += warps)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        load16<DT, VEC>(v[0][h], row + u * UNIT_K + 64 * h, have - u * UNIT_K - 64 * h, m);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) a = fmaxf(a, fabsf(v[0][h][i]));
+      }
+  } else {
+#pragma unroll
+    for (int n = 0; n < NU; ++n) {
+      const int64_t u = (int64_t)(rank + ctas * (warp + warps * n));
+#pragma unroll
+      for (int h = 0; h < 2; ++h) load16<DT, VEC>(v[n][h], row + u * UNIT_K + 64 * h, have - u * UNIT_K - 64 * h, m);
+    }
+#pragma unroll
+    for (int n = 0; n < NU; ++n)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) a = fmaxf(a, fabsf(v[n][h][i]));
+  }
+  a = max_over_cluster(mx, a, warp, lane, warps, ctas, rank);
   const int t = nv_row_exp(fminf(a, type_max<DT>()));
   const float down = pow2_neg(t);
-  if (warp == 0 && (lane & 3) == 0 && r >= 0) *reinterpret_cast<float*>(buf + s.factors + (size_t)r * 4) = __uint_as_float((uint32_t)(t + 127) << 23);
-  for (int64_t u = warp; u < s.units; u += ONE ? s.units : (int64_t)warps) {
-    if constexpr (!ONE) load_unit<DT, VEC>(v, row, u * UNIT_K, s.K, st, lane);
-    uint32_t sc;
-    const uint4 c = encode_nv<DT>(v, down, sc);
+  if (rank == 0 && warp == 0 && (lane & 3) == 0 && r >= 0) *reinterpret_cast<float*>(buf + s.factors + (size_t)r * 4) = __uint_as_float((uint32_t)(t + 127) << 23);
+  auto encode = [&](float (&w)[2][16], int64_t u) {
     const Unit x = unit_at<false, SDQ_FMT_NVFP4>(buf, g, u, s.kblocks, lane);
-    if (r >= 0) put_codes(x, c);
+    uint32_t sc[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint2 c = encode_nv<DT>(w[h], down, sc[h]);
+      if (r >= 0) put_codes(x, h, c);
+    }
     put_scales<SDQ_FMT_NVFP4>(x, sc, lane, r >= 0);
+  };
+  if constexpr (LONG) {
+    for (int64_t u = warp; u < s.units; u += warps) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) load16<DT, VEC>(v[0][h], row + u * UNIT_K + 64 * h, have - u * UNIT_K - 64 * h, m);
+      encode(v[0], u);
+    }
+  } else {
+#pragma unroll
+    for (int n = 0; n < NU; ++n) {
+      const int64_t u = (int64_t)(rank + ctas * (warp + warps * n));
+      if (u < s.units) encode(v[n], u);
+    }
   }
 }
 
@@ -303,34 +443,33 @@ template <int FMT, bool EXPERTS>
 __global__ void __launch_bounds__(32 * Q_WARPS)
 mx4_import_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, const float* __restrict__ factor, Shape s, uint8_t* __restrict__ buf)
 {
-  constexpr int PER = FMT == SDQ_FMT_NVFP4 ? 2 : 1;
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) ptx::griddep_launch_dependents();
   ptx::griddep_wait();
   const int64_t g = blockIdx.x, r = element_row<EXPERTS>(g, s.R, s.tiles, lane);
   const int64_t kb = (s.K + 1) / 2, nb = FMT == SDQ_FMT_NVFP4 ? (s.K + 15) / 16 : (s.K + 31) / 32;
   for (int64_t u = (int64_t)blockIdx.y * Q_WARPS + warp; u < s.units; u += (int64_t)gridDim.y * Q_WARPS) {
-    uint32_t w[4] = {0, 0, 0, 0}, sc = 0;
-    if (r >= 0) {
-      const int64_t b0 = u * 64 + (lane & 3) * 16;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int64_t b = b0 + i;
-        if (b < kb) {
-          uint32_t x = codes[r * kb + b];
-          if (2 * b + 1 == s.K) x &= 15u;
-          w[i / 4] |= x << (8 * (i % 4));
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < PER; ++i) {
-        const int64_t b = (u * 4 + (lane & 3)) * PER + i;
-        if (b < nb) sc |= (uint32_t)scales[r * nb + b] << (8 * i);
-      }
-    }
     const Unit x = unit_at<EXPERTS, FMT>(buf, g, u, s.kblocks, lane);
     const bool on = EXPERTS || r >= 0;
-    if (on) put_codes(x, make_uint4(w[0], w[1], w[2], w[3]));
+    uint32_t sc[2] = {0, 0};
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      uint32_t w[2] = {0, 0};
+      if (r >= 0) {
+        const int64_t b0 = u * 64 + 32 * h + (lane & 3) * 8, sb = FMT == SDQ_FMT_NVFP4 ? u * 8 + 4 * h + (lane & 3) : u * 4 + 2 * h + ((lane >> 1) & 1);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int64_t b = b0 + i;
+          if (b < kb) {
+            uint32_t c = codes[r * kb + b];
+            if (2 * b + 1 == s.K) c &= 15u;
+            w[i / 4] |= c << (8 * (i % 4));
+          }
+        }
+        if (sb < nb) sc[h] = scales[r * nb + sb];
+      }
+      if (on) put_codes(x, h, make_uint2(w[0], w[1]));
+    }
     put_scales<FMT>(x, sc, lane, on);
   }
   if (FMT == SDQ_FMT_NVFP4 && blockIdx.y == 0 && warp == 0 && (lane & 3) == 0 && r >= 0)
@@ -340,7 +479,6 @@ template <int FMT, bool EXPERTS>
 __global__ void __launch_bounds__(32 * Q_WARPS)
 mx4_export_kernel(uint8_t* __restrict__ buf, Shape s, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales, float* __restrict__ factor)
 {
-  constexpr int PER = FMT == SDQ_FMT_NVFP4 ? 2 : 1;
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) ptx::griddep_launch_dependents();
   ptx::griddep_wait();
@@ -349,17 +487,14 @@ mx4_export_kernel(uint8_t* __restrict__ buf, Shape s, uint8_t* __restrict__ code
   const int64_t kb = (s.K + 1) / 2, nb = FMT == SDQ_FMT_NVFP4 ? (s.K + 15) / 16 : (s.K + 31) / 32;
   for (int64_t u = (int64_t)blockIdx.y * Q_WARPS + warp; u < s.units; u += (int64_t)gridDim.y * Q_WARPS) {
     const Unit x = unit_at<EXPERTS, FMT>(buf, g, u, s.kblocks, lane);
-    const uint4 c = get_codes(x);
-    const uint32_t w[4] = {c.x, c.y, c.z, c.w}, sc = get_scales<FMT>(x, lane);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int64_t b = u * 64 + (lane & 3) * 16 + i;
-      if (b < kb) codes[r * kb + b] = (uint8_t)(w[i / 4] >> (8 * (i % 4)));
-    }
+    for (int h = 0; h < 2; ++h) {
+      const uint2 c = get_codes(x, h);
+      const int64_t b0 = u * 64 + 32 * h + (lane & 3) * 8, sb = FMT == SDQ_FMT_NVFP4 ? u * 8 + 4 * h + (lane & 3) : u * 4 + 2 * h + ((lane >> 1) & 1);
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int64_t b = (u * 4 + (lane & 3)) * PER + i;
-      if (b < nb) scales[r * nb + b] = (uint8_t)(sc >> (8 * i));
+      for (int i = 0; i < 8; ++i)
+        if (b0 + i < kb) codes[r * kb + b0 + i] = (uint8_t)((i < 4 ? c.x : c.y) >> (8 * (i % 4)));
+      if (sb < nb) scales[r * nb + sb] = (uint8_t)get_scale<FMT>(x, h, lane);      // (MXFP4: both lanes of a pair write the same)
     }
   }
   if (FMT == SDQ_FMT_NVFP4 && factor && blockIdx.y == 0 && warp == 0 && (lane & 3) == 0) factor[r] = *reinterpret_cast<const float*>(buf + s.factors + (size_t)r * 4);
@@ -383,7 +518,7 @@ __global__ void __launch_bounds__(32 * Q_WARPS)
 mx4_dequantize_kernel(uint8_t* __restrict__ buf, Shape s, typename Elem<DT>::type* __restrict__ out)
 {
   using T = typename Elem<DT>::type;
-  constexpr int PER = 16 / sizeof(T);
+  constexpr int W = 16 * sizeof(T) / 4;
   __shared__ __align__(16) uint8_t stage[VEC ? 16 : Q_WARPS * Stage<DT>::BYTES];
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) ptx::griddep_launch_dependents();
@@ -393,61 +528,37 @@ mx4_dequantize_kernel(uint8_t* __restrict__ buf, Shape s, typename Elem<DT>::typ
   float f = 1.0f;
   if (FMT == SDQ_FMT_NVFP4 && r >= 0) f = *reinterpret_cast<const float*>(buf + s.factors + (size_t)r * 4);
   for (int64_t u = (int64_t)blockIdx.y * (blockDim.x >> 5) + warp; u < s.units; u += (int64_t)gridDim.y * (blockDim.x >> 5)) {
-    float v[32];
-    if (r >= 0) {
-      const Unit x = unit_at<EXPERTS, FMT>(buf, g, u, s.kblocks, lane);
-      const uint4 c = get_codes(x);
-      const uint32_t sc = get_scales<FMT>(x, lane);
-      values8(c.x, v);
-      values8(c.y, v + 8);
-      values8(c.z, v + 16);
-      values8(c.w, v + 24);
+    const Unit x = unit_at<EXPERTS, FMT>(buf, g, u, s.kblocks, lane);
+    T* row = r < 0 ? nullptr : out + r * s.ld + u * UNIT_K;
+    uint2 c[2];
+    uint32_t sc[2];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const float m = FMT == SDQ_FMT_MXFP4 ? e8m0_value(sc) : e4m3_value((sc >> (8 * h)) & 0xFFu);
+    for (int h = 0; h < 2; ++h) {
+      c[h] = make_uint2(0, 0);
+      sc[h] = 0;
+      if (r >= 0) { c[h] = get_codes(x, h); sc[h] = get_scale<FMT>(x, h, lane); }
+    }
 #pragma unroll
-        for (int i = 16 * h; i < 16 * h + 16; ++i) v[i] = FMT == SDQ_FMT_MXFP4 ? v[i] * m : v[i] * m * f;
+    for (int h = 0; h < 2; ++h) {
+      float v[16];
+      values8(c[h].x, v);
+      values8(c[h].y, v + 8);
+      const float m = FMT == SDQ_FMT_MXFP4 ? e8m0_value(sc[h]) : e4m3_value(sc[h]);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) v[i] = FMT == SDQ_FMT_MXFP4 ? v[i] * m : v[i] * m * f;
+      uint32_t w[W];
+      pack16<DT>(w, v);
+      const int64_t k = 64 * h + 16 * (lane & 3);
+      if constexpr (VEC) {
+        constexpr int PER = 32 / sizeof(T);
+#pragma unroll
+        for (int i = 0; i < W / 8; ++i)
+          if (row && u * UNIT_K + k + i * PER < s.K) st32(row + k + i * PER, *reinterpret_cast<const uint32_t(*)[8]>(w + 8 * i));
+      } else {
+        stage16<DT>(st + (lane >> 2) * Stage<DT>::PITCH, (uint32_t)((uintptr_t)row & 15), (uint32_t)k, w);
       }
     }
-    uint4 raw[32 / PER];
-#pragma unroll
-    for (int i = 0; i < 32 / PER; ++i) {
-      uint32_t w[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if constexpr (DT == SDQ_FP32) w[j] = __float_as_uint(v[4 * i + j]);
-        else if constexpr (DT == SDQ_BF16) {
-          const __nv_bfloat162 b = __floats2bfloat162_rn(v[8 * i + 2 * j], v[8 * i + 2 * j + 1]);
-          w[j] = *reinterpret_cast<const uint32_t*>(&b);
-        } else {
-          const __half2 b = __floats2half2_rn(v[8 * i + 2 * j], v[8 * i + 2 * j + 1]);
-          w[j] = *reinterpret_cast<const uint32_t*>(&b);
-        }
-      }
-      raw[i] = make_uint4(w[0], w[1], w[2], w[3]);
-    }
-    T* row = r < 0 ? nullptr : out + r * s.ld;
-    if constexpr (VEC) {
-      const int64_t k = u * UNIT_K + 32 * (lane & 3);
-#pragma unroll
-      for (int i = 0; i < 32 / PER; ++i)
-        if (row && k + i * PER < s.K) *reinterpret_cast<uint4*>(row + k + i * PER) = raw[i];
-    } else {
-      uint4* sp = reinterpret_cast<uint4*>(st + (lane >> 2) * Stage<DT>::PITCH + (lane & 3) * 32 * sizeof(T));
-#pragma unroll
-      for (int i = 0; i < 32 / PER; ++i) sp[i] = raw[i];
-      __syncwarp();
-#pragma unroll
-      for (int q = 0; q < 8; ++q) {
-        T* p = reinterpret_cast<T*>(__shfl_sync(0xffffffffu, (unsigned long long)(uintptr_t)row, 4 * q));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int64_t k = u * UNIT_K + 32 * i + lane;
-          if (p && k < s.K) p[k] = *reinterpret_cast<const T*>(st + q * Stage<DT>::PITCH + (32 * i + lane) * sizeof(T));
-        }
-      }
-      __syncwarp();
-    }
+    if constexpr (!VEC) store_staged<DT>(st, row, (int)min((int64_t)UNIT_K, s.K - u * UNIT_K) * (int)sizeof(T), lane);
   }
 }
 
@@ -455,30 +566,36 @@ mx4_dequantize_kernel(uint8_t* __restrict__ buf, Shape s, typename Elem<DT>::typ
 static Shape shape_of(int64_t E, int64_t R, int64_t K, int64_t ld, int fmt) {
   const Dims d = dims(E, R, K, fmt);
   Shape s;
-  s.R = R; s.K = K; s.ld = ld; s.tiles = d.tiles; s.kblocks = d.kblocks; s.units = E ? d.kblocks : 2 * d.kblocks;
+  s.R = R; s.rows = (E ? E : 1) * R; s.K = K; s.ld = ld; s.tiles = d.tiles; s.kblocks = d.kblocks; s.units = E ? d.kblocks : 2 * d.kblocks;
   s.factors = d.factors;
   return s;
 }
 template <typename... P, typename... A>
-static sdq_status_t launch(void (*kern)(P...), dim3 grid, unsigned threads, void* stream, A... args) {
+static sdq_status_t launch_cluster(unsigned cluster, void (*kern)(P...), dim3 grid, unsigned threads, void* stream, A... args) {
   cudaLaunchConfig_t lc = {};
   lc.gridDim = grid;
   lc.blockDim = dim3(threads);
   lc.stream = (cudaStream_t)stream;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = 1;
+  attr[1].val.clusterDim.y = cluster;
+  attr[1].val.clusterDim.z = 1;
   lc.attrs = attr;
-  lc.numAttrs = 1;
+  lc.numAttrs = cluster ? 2 : 1;
   return launch_status(cudaLaunchKernelEx(&lc, kern, args...));
 }
+template <typename... P, typename... A>
+static sdq_status_t launch(void (*kern)(P...), dim3 grid, unsigned threads, void* stream, A... args) { return launch_cluster(0, kern, grid, threads, stream, args...); }
 // 8-row groups, one a thread block along x: linear: those that hold rows; experts: of all padded rows
 static int64_t groups_of(int64_t E, const Shape& s) { return E ? E * s.tiles * 16 : (s.R + 7) / 8; }
 static unsigned blocks_along_k(const Shape& s, int warps) { return (unsigned)((s.units + warps - 1) / warps < 65535 ? (s.units + warps - 1) / warps : 65535); }
-// rows a vector access of 16 bytes fits
+// rows whose elements lie on 32-byte boundaries
 static bool vectors_fit(const void* p, int64_t ld, int64_t K, int32_t dtype, bool one_row) {
-  const int64_t per = 16 / (int64_t)dtype_bytes(dtype);
-  return ((uintptr_t)p & 15) == 0 && K % per == 0 && (ld % per == 0 || one_row);
+  const int64_t per = 32 / (int64_t)dtype_bytes(dtype);
+  return ((uintptr_t)p & 31) == 0 && K % per == 0 && (ld % per == 0 || one_row);
 }
 static void describe(sdq_mx4_t* out, void* buf, int64_t E, int64_t R, int64_t K, int fmt) {
   const Dims d = dims(E, R, K, fmt);
@@ -493,11 +610,14 @@ static sdq_status_t quantize(const void* X, int64_t E, const Shape& s, int fmt, 
   const int64_t groups = groups_of(E, s);
   if (groups > 0x7FFFFFFF) return SDQ_ERR_SHAPE;
   if (fmt == SDQ_FMT_NVFP4) {
-    const int64_t warps = vec ? NvWarps<DT, true>::value : NvWarps<DT, false>::value;
-    const unsigned threads = 32u * (unsigned)(s.units < warps ? s.units : warps);
-    auto nv = [&](auto kern) { return launch(kern, dim3((unsigned)groups), threads, stream, x, s, buf); };
-    if (s.units <= warps) return vec ? nv(nv4_quantize_kernel<DT, true, true>) : nv(nv4_quantize_kernel<DT, false, true>);
-    return vec ? nv(nv4_quantize_kernel<DT, true, false>) : nv(nv4_quantize_kernel<DT, false, false>);
+    // one unit a warp where the CTAs of a cluster have as many warps, else two; short rows take fewer warps
+    const int nu = s.units <= NV_CTAS * Q_WARPS ? 1 : 2;
+    const int64_t warps = (s.units + nu - 1) / nu, ctas = (warps + Q_WARPS - 1) / Q_WARPS;
+    if (ctas > NV_CTAS) return vec ? launch(nv4_quantize_kernel<DT, true, 1, true>, dim3((unsigned)groups), 32 * Q_WARPS, stream, x, s, buf)
+                                   : launch(nv4_quantize_kernel<DT, false, 1, true>, dim3((unsigned)groups), 32 * Q_WARPS, stream, x, s, buf);
+    auto nv = [&](auto kern) { return launch_cluster((unsigned)ctas, kern, dim3((unsigned)groups, (unsigned)ctas), 32u * (unsigned)((warps + ctas - 1) / ctas), stream, x, s, buf); };
+    if (nu == 1) return vec ? nv(nv4_quantize_kernel<DT, true, 1, false>) : nv(nv4_quantize_kernel<DT, false, 1, false>);
+    return vec ? nv(nv4_quantize_kernel<DT, true, 2, false>) : nv(nv4_quantize_kernel<DT, false, 2, false>);
   }
   const dim3 grid((unsigned)groups, blocks_along_k(s, Q_WARPS));
   auto go = [&](auto kern) { return launch(kern, grid, 32 * Q_WARPS, stream, x, s, rule, buf); };
