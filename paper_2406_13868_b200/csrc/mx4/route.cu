@@ -1,9 +1,10 @@
 // Router of an expert layer: logits of every token over the experts, scores, the k best and their weights, in one launch.
 //
-// A cluster takes a group of tokens; its CTAs share the experts, a warp forms the logits of one expert for all tokens of the group (the
-// expert's row is read once for them).  Products of 16-bit operands are exact in fp32, eight are summed there, everything behind that in
-// 64 bits: which expert is chosen then hangs on the inputs, not on the order of a sum.  Each token's logits are gathered in the shared
-// memory of one CTA, where one warp scores and chooses.
+// A cluster takes a group of tokens; its CTAs share the experts, and K where there are few of them.  Each token's logits are gathered in the
+// shared memory of one CTA, which scores and chooses.  Which expert is chosen must not hang on the order of a sum: products of 16-bit
+// operands are exact in fp32, 32 of them are summed there, by the tensor core (mma.sync: sixteen experts x eight tokens, a shape that
+// this size of problem fills, where a tcgen05 tile would be all padding), and everything behind that in 64 bits.  fp32 operands go through
+// ordinary multiplications, eight to a sum.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -69,17 +70,184 @@ struct RouteParams {
   int32_t* ids;
   float* weights;
   int64_t T, H, ldx, ldw;
-  int32_t E, k, sigmoid, renorm, elements;   // elements: doubles of a logit row in shared memory
+  int32_t E, k, sigmoid, renorm, elements, splits;   // elements: doubles of a logit row in shared memory; splits: parts of K (16-bit operands)
   float scale;
 };
 
-// G tokens a cluster
+// one token's scores, choices and weights, by all warps of the CTA.  score: [E] logits, scratch behind; key: [E]; red: [2 ROUTE_WARPS]
+__device__ __forceinline__ double block_reduce(double v, bool sum, double* red) {
+  const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+#pragma unroll
+  for (int o = 16; o; o >>= 1) {
+    const double u = __shfl_xor_sync(0xffffffffu, v, o);
+    v = sum ? v + u : fmax(v, u);
+  }
+  if (lane == 0) red[warp] = v;
+  __syncthreads();
+  v = red[0];
+  for (int w = 1; w < ROUTE_WARPS; ++w) v = sum ? v + red[w] : fmax(v, red[w]);
+  return v;
+}
+__device__ __forceinline__ void choose(const RouteParams& p, int64_t t, double* score, long long* key, double* red) {
+  const uint32_t tid = threadIdx.x, lane = tid & 31;
+  constexpr int THREADS = 32 * ROUTE_WARPS;
+  // scores: softmax over all experts, or sigmoid
+  double sum = 1.0;
+  if (!p.sigmoid) {
+    double top = -INFINITY;
+    for (int e = (int)tid; e < p.E; e += THREADS) top = fmax(top, score[e]);
+    top = block_reduce(top, false, red);
+    sum = 0.0;
+    for (int e = (int)tid; e < p.E; e += THREADS) { const double v = exp(score[e] - top); sum += v; score[e] = v; }
+    sum = block_reduce(sum, true, red + ROUTE_WARPS);
+  }
+  for (int e = (int)tid; e < p.E; e += THREADS) {
+    const double v = p.sigmoid ? 1.0 / (1.0 + exp(-score[e])) : score[e] / sum;
+    score[e] = v;
+    key[e] = rank_key(p.bias ? v + (double)p.bias[e] : v);
+  }
+  __syncthreads();
+  if (tid >= 32) return;
+  // k times the largest key that is left, of equal ones the lowest index; every lane keeps the best of its own
+  constexpr long long NONE = (long long)0x8000000000000000ull;
+  long long best = NONE;
+  int at = 0x7FFFFFFF;
+  auto scan = [&]() {
+    best = NONE;
+    at = 0x7FFFFFFF;
+    for (int e = (int)lane; e < p.E; e += 32)
+      if (key[e] > best) { best = key[e]; at = e; }
+  };
+  scan();
+  double total = 0.0, mine = 0.0;
+  int my_id = 0;
+  for (int j = 0; j < p.k; ++j) {
+    const int hi = (int)(best >> 32), top = __reduce_max_sync(0xffffffffu, hi);
+    const uint32_t lo = hi == top ? (uint32_t)best : 0u, low = __reduce_max_sync(0xffffffffu, lo);
+    const int win = __reduce_min_sync(0xffffffffu, hi == top && lo == low ? at : 0x7FFFFFFF);
+    const double v = score[win];
+    total += v;
+    if ((int)lane == j) { mine = v; my_id = win; }
+    if (win == at) { key[win] = NONE; scan(); }
+  }
+  if ((int)lane < p.k) {
+    p.ids[t * p.k + lane] = my_id;
+    p.weights[t * p.k + lane] = (float)((p.renorm ? mine / total : mine) * (double)p.scale);
+  }
+}
+
+// ---- 16-bit operands ------------------------------------------------------------------------------------------------------------
+constexpr int ROUTE_TOKENS = 8;                     // of a cluster: an MMA's columns, and one for each CTA
+template <int DT>
+__device__ __forceinline__ void mma_16x8x16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  if constexpr (DT == SDQ_BF16)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// eight consecutive 16-bit elements of a row, `n` of which exist
+template <bool VEC>
+__device__ __forceinline__ uint4 load8_raw(const uint16_t* p, int64_t n) {
+  uint32_t w[4] = {0, 0, 0, 0};
+  if constexpr (VEC) {
+    if (n > 0) return __ldg(reinterpret_cast<const uint4*>(p));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) w[i / 2] |= (uint32_t)p[i] << (16 * (i & 1));
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// The warps of a CTA share its K.  The K of the operands' fragments is permuted alike, which a sum does not see: lane 4 r + c loads K 8 c .. + 7 of a
+// chunk of 32 of rows r and r + 8, one access each, and its words 0, 1 and 2, 3 are the fragments of two MMAs.
+constexpr int ROUTE_PAIR = 2;                       // tiles of sixteen experts at a time
+template <int DT, bool VEC>
+__global__ void __launch_bounds__(32 * ROUTE_WARPS)
+moe_route_mma_kernel(const __grid_constant__ RouteParams p)
+{
+  extern __shared__ double s_logit[];               // [K splits][E], keys [E], sums of the warps
+  const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, c8 = (lane & 3) * 8;
+  const uint32_t rank = ptx::cluster_ctarank();
+  const int64_t t0 = (int64_t)(blockIdx.x / ROUTE_CTAS) * ROUTE_TOKENS;
+  long long* key = reinterpret_cast<long long*>(s_logit + (size_t)p.splits * p.elements);
+  double* red = reinterpret_cast<double*>(key + p.elements);          // [warp][tile of the pair][16 experts][8 tokens]
+  const uint16_t *X = reinterpret_cast<const uint16_t*>(p.x), *W = reinterpret_cast<const uint16_t*>(p.w);
+  // this CTA's tiles and K
+  const int tiles = (p.E + 15) / 16, split = p.splits > 1 ? (int)rank / tiles : 0, step = p.splits > 1 ? tiles : ROUTE_CTAS;
+  const int64_t chunks = (p.H + 31) / 32, parts = (int64_t)p.splits * ROUTE_WARPS, part = (int64_t)split * ROUTE_WARPS + warp;
+  const int64_t h0 = part * chunks / parts * 32, h1 = (part + 1) * chunks / parts * 32;
+  if (tid == 0) ptx::griddep_launch_dependents();
+  ptx::griddep_wait();
+  ptx::cluster_sync();                              // (all CTAs have started: their shared memory may be written)
+  const bool token = t0 + r < p.T;
+  const uint16_t* x = X + (t0 + r) * p.ldx + c8;
+  for (int tile = (int)rank - split * tiles; split < p.splits && tile < tiles; tile += ROUTE_PAIR * step) {
+    const uint16_t* w[ROUTE_PAIR][2];
+    bool have[ROUTE_PAIR][2];
+    double acc[ROUTE_PAIR][4];
+#pragma unroll
+    for (int i = 0; i < ROUTE_PAIR; ++i) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int e = (tile + i * step) * 16 + (int)r + 8 * j;
+        have[i][j] = e < p.E;
+        w[i][j] = W + (int64_t)(have[i][j] ? e : 0) * p.ldw + c8;
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[i][j] = 0.0;
+    }
+#pragma unroll 4
+    for (int64_t h = h0; h < h1; h += 32) {
+      const int64_t n = p.H - h - c8;
+      const uint4 b = load8_raw<VEC>(x + h, token ? n : 0);
+#pragma unroll
+      for (int i = 0; i < ROUTE_PAIR; ++i) {
+        const uint4 lo = load8_raw<VEC>(w[i][0] + h, have[i][0] ? n : 0), hi = load8_raw<VEC>(w[i][1] + h, have[i][1] ? n : 0);
+        float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        mma_16x8x16<DT>(d, lo.x, hi.x, lo.y, hi.y, b.x, b.y);
+        mma_16x8x16<DT>(d, lo.z, hi.z, lo.w, hi.w, b.z, b.w);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] += (double)d[j];
+      }
+    }
+    // accumulator j of lane 4 r + c: expert r + 8 (j / 2), token 2 c + j % 2
+    __syncthreads();                                // (the sums of the tiles in front have been read)
+#pragma unroll
+    for (int i = 0; i < ROUTE_PAIR; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) red[((warp * ROUTE_PAIR + i) * 16 + r + 8 * (j >> 1)) * 8 + 2 * (lane & 3) + (j & 1)] = acc[i][j];
+    __syncthreads();
+    for (int q = (int)tid; q < ROUTE_PAIR * 128; q += 32 * ROUTE_WARPS) {
+      const int e = (tile + (q >> 7) * step) * 16 + ((q >> 3) & 15);
+      double s = 0.0;
+#pragma unroll
+      for (int v = 0; v < ROUTE_WARPS; ++v) s += red[v * ROUTE_PAIR * 128 + q];
+      if (e < p.E) store_to_cta(s_logit + (size_t)split * p.elements + e, (uint32_t)q & 7u, s);
+    }
+  }
+  ptx::cluster_sync();
+  if (t0 + rank >= p.T) return;                     // token `rank` of the group is this CTA's
+  if (p.splits > 1) {
+    for (int e = (int)tid; e < p.E; e += 32 * ROUTE_WARPS) {
+      double s = s_logit[e];
+      for (int v = 1; v < p.splits; ++v) s += s_logit[(size_t)v * p.elements + e];
+      s_logit[e] = s;
+    }
+    __syncthreads();
+  }
+  choose(p, t0 + rank, s_logit, key, red);
+}
+
+// ---- fp32 operands: G tokens a cluster --------------------------------------------------------------------------------------------
 template <int DT, int G, bool VEC>
 __global__ void __launch_bounds__(32 * ROUTE_WARPS)
 moe_route_kernel(const __grid_constant__ RouteParams p)
 {
   using T = typename RouteElem<DT>::type;
-  extern __shared__ double s_logit[];        // [tokens of this CTA][E], then as many keys
+  static_assert(G <= ROUTE_CTAS);
+  extern __shared__ double s_logit[];        // [E], keys [E], sums of the warps
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   uint32_t ctas;
   asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(ctas));
@@ -110,60 +278,18 @@ moe_route_kernel(const __grid_constant__ RouteParams p)
 #pragma unroll
     for (int g = 0; g < G; ++g) {
       const double l = warp_sum(acc[g]);
-      if (lane == 0) store_to_cta(s_logit + (size_t)(g / ctas) * p.elements + e, (uint32_t)g % ctas, l);
+      if (lane == 0) store_to_cta(s_logit + e, (uint32_t)g, l);
     }
   }
   ptx::cluster_sync();
-  // token g of the group: CTA g % ctas, warp g / ctas
-  const int g = (int)(warp * ctas + rank);
-  if (g >= G || t0 + g >= p.T) return;
-  double* score = s_logit + (size_t)warp * p.elements;
-  long long* key = reinterpret_cast<long long*>(s_logit + (size_t)((G + ctas - 1) / ctas) * p.elements) + (size_t)warp * p.elements;
-  // scores: softmax over all experts, or sigmoid
-  double sum = 1.0;
-  if (!p.sigmoid) {
-    double top = -INFINITY;
-    for (int e = (int)lane; e < p.E; e += 32) top = fmax(top, score[e]);
-#pragma unroll
-    for (int o = 16; o; o >>= 1) top = fmax(top, __shfl_xor_sync(0xffffffffu, top, o));
-    sum = 0.0;
-    for (int e = (int)lane; e < p.E; e += 32) { const double v = exp(score[e] - top); sum += v; score[e] = v; }
-    sum = warp_sum(sum);
-  }
-  for (int e = (int)lane; e < p.E; e += 32) {
-    const double v = p.sigmoid ? 1.0 / (1.0 + exp(-score[e])) : score[e] / sum;
-    score[e] = v;
-    key[e] = rank_key(p.bias ? v + (double)p.bias[e] : v);
-  }
-  double total = 0.0, mine = 0.0;
-  int my_id = 0;
-  for (int j = 0; j < p.k; ++j) {
-    // the largest key that is left, of equal ones the lowest index
-    long long best = (long long)0x8000000000000000ull;
-    int at = 0x7FFFFFFF;
-    for (int e = (int)lane; e < p.E; e += 32)
-      if (key[e] > best) { best = key[e]; at = e; }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) {
-      const long long b = __shfl_xor_sync(0xffffffffu, best, o);
-      const int a = __shfl_xor_sync(0xffffffffu, at, o);
-      if (b > best || (b == best && a < at)) { best = b; at = a; }
-    }
-    const double v = score[at];
-    total += v;
-    if ((int)lane == j) { mine = v; my_id = at; }
-    __syncwarp();
-    if (lane == 0) key[at] = (long long)0x8000000000000000ull;
-    __syncwarp();
-  }
-  if ((int)lane < p.k) {
-    p.ids[(t0 + g) * p.k + lane] = my_id;
-    p.weights[(t0 + g) * p.k + lane] = (float)((p.renorm ? mine / total : mine) * (double)p.scale);
-  }
+  // token `rank` of the group is this CTA's
+  if (rank >= G || t0 + rank >= p.T) return;
+  long long* key = reinterpret_cast<long long*>(s_logit + p.elements);
+  choose(p, t0 + rank, s_logit, key, reinterpret_cast<double*>(key + p.elements));
 }
 
-template <int DT, int G>
-static sdq_status_t route(const RouteParams& p, bool vec, void* stream) {
+template <typename K>
+static sdq_status_t launch_route(K kern, const RouteParams& p, int64_t groups, size_t smem, void* stream) {
   cudaLaunchConfig_t lc = {};
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -172,15 +298,29 @@ static sdq_status_t route(const RouteParams& p, bool vec, void* stream) {
   attr[1].val.clusterDim.x = ROUTE_CTAS;
   attr[1].val.clusterDim.y = 1;
   attr[1].val.clusterDim.z = 1;
-  const int64_t groups = (p.T + G - 1) / G;
   if (groups > 0x7FFFFFFF / ROUTE_CTAS) return SDQ_ERR_SHAPE;
   lc.gridDim = dim3((unsigned)groups * ROUTE_CTAS);
   lc.blockDim = dim3(32 * ROUTE_WARPS);
-  lc.dynamicSmemBytes = (size_t)((G + ROUTE_CTAS - 1) / ROUTE_CTAS) * p.elements * 16;
+  lc.dynamicSmemBytes = smem;
   lc.stream = (cudaStream_t)stream;
   lc.attrs = attr;
   lc.numAttrs = 2;
-  return launch_status(vec ? cudaLaunchKernelEx(&lc, moe_route_kernel<DT, G, true>, p) : cudaLaunchKernelEx(&lc, moe_route_kernel<DT, G, false>, p));
+  return launch_status(cudaLaunchKernelEx(&lc, kern, p));
+}
+template <int DT>
+static sdq_status_t route16(RouteParams p, bool vec, void* stream) {
+  static_assert(ROUTE_TOKENS == ROUTE_CTAS);
+  const int tiles = (p.E + 15) / 16;
+  p.splits = tiles < ROUTE_CTAS ? ROUTE_CTAS / tiles : 1;
+  const size_t smem = ((size_t)p.splits + 1) * p.elements * 8 + (size_t)ROUTE_WARPS * ROUTE_PAIR * 128 * 8;
+  const int64_t groups = (p.T + ROUTE_TOKENS - 1) / ROUTE_TOKENS;
+  return vec ? launch_route(moe_route_mma_kernel<DT, true>, p, groups, smem, stream) : launch_route(moe_route_mma_kernel<DT, false>, p, groups, smem, stream);
+}
+template <int G>
+static sdq_status_t route32(const RouteParams& p, bool vec, void* stream) {
+  const size_t smem = 2 * (size_t)p.elements * 8 + 2 * ROUTE_WARPS * 8;
+  const int64_t groups = (p.T + G - 1) / G;
+  return vec ? launch_route(moe_route_kernel<SDQ_FP32, G, true>, p, groups, smem, stream) : launch_route(moe_route_kernel<SDQ_FP32, G, false>, p, groups, smem, stream);
 }
 
 }  // namespace mx4
@@ -199,9 +339,8 @@ extern "C" sdq_status_t sdq_moe_route(const void* X, int32_t dtype, int64_t T, i
   const size_t es = dtype_bytes(dtype);
   if ((uintptr_t)X % es || (uintptr_t)Wr % es || (uintptr_t)bias % 4 || (uintptr_t)ids % 4 || (uintptr_t)weights % 4) return SDQ_ERR_ALIGNMENT;
   const bool vec = !((uintptr_t)X & 15) && !((uintptr_t)Wr & 15) && H % 8 == 0 && (ldx % 8 == 0 || T == 1) && (ldw % 8 == 0 || E == 1);
-  const RouteParams p = {X, Wr, bias, ids, weights, T, H, ldx, ldw, (int32_t)E, k, scoring == SDQ_ROUTE_SIGMOID, renorm != 0, (int32_t)(E + 1) / 2 * 2, scale};
-  const bool one = T <= 8;
-  if (dtype == SDQ_BF16) return one ? route<SDQ_BF16, 1>(p, vec, stream) : route<SDQ_BF16, 4>(p, vec, stream);
-  if (dtype == SDQ_FP16) return one ? route<SDQ_FP16, 1>(p, vec, stream) : route<SDQ_FP16, 4>(p, vec, stream);
-  return one ? route<SDQ_FP32, 1>(p, vec, stream) : route<SDQ_FP32, 4>(p, vec, stream);
+  const RouteParams p = {X, Wr, bias, ids, weights, T, H, ldx, ldw, (int32_t)E, k, scoring == SDQ_ROUTE_SIGMOID, renorm != 0, (int32_t)(E + 1) / 2 * 2, 1, scale};
+  if (dtype == SDQ_BF16) return route16<SDQ_BF16>(p, vec, stream);
+  if (dtype == SDQ_FP16) return route16<SDQ_FP16>(p, vec, stream);
+  return T <= 8 ? route32<1>(p, vec, stream) : route32<4>(p, vec, stream);      // (few tokens: more clusters)
 }

@@ -24,7 +24,7 @@ def test_no_remote_shared_memory_before_the_cluster_has_started(bodies):
     """distributed shared memory may be touched only when all CTAs of the cluster are known to have started, and no CTA leaves before the others
     are through with its own"""
     remote = {n: b for n, b in bodies.items() if REMOTE.search(b)}
-    assert {"mx4_linear_narrow_kernel", "mx4_linear_wide_kernel", "moe_route_kernel", "moe_up_kernel", "moe_down_kernel"} <= set(remote)
+    assert {"mx4_linear_narrow_kernel", "mx4_linear_wide_kernel", "moe_route_kernel", "moe_route_mma_kernel", "moe_up_kernel", "moe_down_kernel"} <= set(remote)
     for n, b in remote.items():
         first, last = REMOTE.search(b).start(), [x.start() for x in REMOTE.finditer(b)][-1]
         syncs = [x.start() for x in re.finditer(r"ptx::cluster_sync\(\)", b)]
@@ -37,7 +37,7 @@ def test_global_memory_is_read_behind_the_wait_for_the_launch_in_front(bodies):
         if n in ("moe_up_kernel", "moe_down_kernel"):
             continue
         wait = b.index("ptx::griddep_wait()")
-        for what in (r"ptx::bulk_g2s\(", r"__ldg\(", r"\bload_unit<", r"get_codes\(", r"put_codes\(", r"codes\[r", r"atomicOr\(", r"\bload8<", r"p\.(?:ids|weights|ws)\b"):
+        for what in (r"ptx::bulk_g2s\(", r"__ldg\(", r"\bload_unit<", r"get_codes\(", r"put_codes\(", r"codes\[r", r"atomicOr\(", r"\bload8<", r"load8_raw<", r"p\.(?:ids|weights|ws)\b"):
             assert all(x.start() > wait for x in re.finditer(what, b)), (n, what)
 
 
