@@ -23,6 +23,9 @@ __device__ __forceinline__ void copy32(uint32_t dst, const void* src, uint32_t b
 __device__ __forceinline__ void commit32(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
+// the two halves of ptx::cluster_sync
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 // position in a ring of `n` slots: barriers 8 bytes apart, data `size` bytes apart; `ph` flips with every lap
 struct Slot {
   uint32_t s, ph, full, empty, at;

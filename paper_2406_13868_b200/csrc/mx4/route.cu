@@ -11,11 +11,12 @@
 #include "../sdq_internal.h"
 #include "../sdq_ptx.cuh"
 #include "layout.h"
+#include "pipe.cuh"
 
 namespace sdq {
 namespace mx4 {
 
-constexpr int ROUTE_WARPS = 8, ROUTE_CTAS = 8;
+constexpr int ROUTE_WARPS = 16, ROUTE_CTAS = 8;
 constexpr int ROUTE_MAX_E = 1024, ROUTE_MAX_K = 32;
 
 template <int DT> struct RouteElem;
@@ -74,35 +75,37 @@ struct RouteParams {
   float scale;
 };
 
-// one token's scores, choices and weights, by all warps of the CTA.  score: [E] logits, scratch behind; key: [E]; red: [2 ROUTE_WARPS]
-__device__ __forceinline__ double block_reduce(double v, bool sum, double* red) {
-  const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-#pragma unroll
-  for (int o = 16; o; o >>= 1) {
-    const double u = __shfl_xor_sync(0xffffffffu, v, o);
-    v = sum ? v + u : fmax(v, u);
-  }
-  if (lane == 0) red[warp] = v;
-  __syncthreads();
-  v = red[0];
-  for (int w = 1; w < ROUTE_WARPS; ++w) v = sum ? v + red[w] : fmax(v, red[w]);
-  return v;
-}
+// one token's scores, choices and weights, by all warps of the CTA.  score: [E] logits; key: [E]; red: scratch of ROUTE_WARPS doubles.
+// A softmax is left undivided where only the order and the ratios of the scores matter.
 __device__ __forceinline__ void choose(const RouteParams& p, int64_t t, double* score, long long* key, double* red) {
-  const uint32_t tid = threadIdx.x, lane = tid & 31;
+  const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   constexpr int THREADS = 32 * ROUTE_WARPS;
-  // scores: softmax over all experts, or sigmoid
-  double sum = 1.0;
+  double inv = 1.0;
   if (!p.sigmoid) {
-    double top = -INFINITY;
-    for (int e = (int)tid; e < p.E; e += THREADS) top = fmax(top, score[e]);
-    top = block_reduce(top, false, red);
-    sum = 0.0;
-    for (int e = (int)tid; e < p.E; e += THREADS) { const double v = exp(score[e] - top); sum += v; score[e] = v; }
-    sum = block_reduce(sum, true, red + ROUTE_WARPS);
+    // the exponentials are formed relative to a number near the largest logit: the fp32 one
+    float top = -INFINITY;
+    for (int e = (int)tid; e < p.E; e += THREADS) top = fmaxf(top, (float)score[e]);
+    const int b = __float_as_int(top + 0.0f), k = __reduce_max_sync(0xffffffffu, b ^ (b >> 31 & 0x7FFFFFFF));
+    float* warps = reinterpret_cast<float*>(red);
+    if (lane == 0) warps[warp] = __int_as_float(k ^ (k >> 31 & 0x7FFFFFFF));
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < ROUTE_WARPS; ++w) top = fmaxf(top, warps[w]);
+    double sum = 0.0;
+    for (int e = (int)tid; e < p.E; e += THREADS) { const double v = exp(score[e] - (double)top); sum += v; score[e] = v; }
+    if (!p.renorm || p.bias) {
+      sum = warp_sum(sum);
+      __syncthreads();
+      if (lane == 0) red[warp] = sum;
+      __syncthreads();
+      sum = red[0];
+#pragma unroll
+      for (int w = 1; w < ROUTE_WARPS; ++w) sum += red[w];
+      inv = 1.0 / sum;
+    }
   }
   for (int e = (int)tid; e < p.E; e += THREADS) {
-    const double v = p.sigmoid ? 1.0 / (1.0 + exp(-score[e])) : score[e] / sum;
+    const double v = p.sigmoid ? 1.0 / (1.0 + exp(-score[e])) : score[e] * inv;
     score[e] = v;
     key[e] = rank_key(p.bias ? v + (double)p.bias[e] : v);
   }
@@ -110,29 +113,51 @@ __device__ __forceinline__ void choose(const RouteParams& p, int64_t t, double* 
   if (tid >= 32) return;
   // k times the largest key that is left, of equal ones the lowest index; every lane keeps the best of its own
   constexpr long long NONE = (long long)0x8000000000000000ull;
-  long long best = NONE;
-  int at = 0x7FFFFFFF;
+  constexpr int KEPT = 8;                             // keys of a lane in registers: 256 experts
+  long long mine[KEPT], best = NONE;
+  int at = 0x7FFFFFFF, my_id = 0;
+  const bool kept = p.E <= 32 * KEPT;
+#pragma unroll
+  for (int i = 0; i < KEPT; ++i) mine[i] = kept && (int)lane + 32 * i < p.E ? key[lane + 32 * i] : NONE;
   auto scan = [&]() {
     best = NONE;
     at = 0x7FFFFFFF;
-    for (int e = (int)lane; e < p.E; e += 32)
-      if (key[e] > best) { best = key[e]; at = e; }
+    if (kept) {
+#pragma unroll
+      for (int i = 0; i < KEPT; ++i)
+        if (mine[i] > best) { best = mine[i]; at = (int)lane + 32 * i; }
+    } else {
+      for (int e = (int)lane; e < p.E; e += 32)
+        if (key[e] > best) { best = key[e]; at = e; }
+    }
   };
   scan();
-  double total = 0.0, mine = 0.0;
-  int my_id = 0;
   for (int j = 0; j < p.k; ++j) {
     const int hi = (int)(best >> 32), top = __reduce_max_sync(0xffffffffu, hi);
-    const uint32_t lo = hi == top ? (uint32_t)best : 0u, low = __reduce_max_sync(0xffffffffu, lo);
-    const int win = __reduce_min_sync(0xffffffffu, hi == top && lo == low ? at : 0x7FFFFFFF);
-    const double v = score[win];
-    total += v;
-    if ((int)lane == j) { mine = v; my_id = win; }
-    if (win == at) { key[win] = NONE; scan(); }
+    const uint32_t who = __ballot_sync(0xffffffffu, hi == top);
+    int win;
+    if ((who & (who - 1)) == 0) {
+      win = __shfl_sync(0xffffffffu, at, __ffs(who) - 1);
+    } else {
+      const uint32_t lo = hi == top ? (uint32_t)best : 0u, low = __reduce_max_sync(0xffffffffu, lo);
+      win = __reduce_min_sync(0xffffffffu, hi == top && lo == low ? at : 0x7FFFFFFF);
+    }
+    if ((int)lane == j) my_id = win;
+    if (win == at) {
+      if (kept) {
+#pragma unroll
+        for (int i = 0; i < KEPT; ++i)
+          if (win == (int)lane + 32 * i) mine[i] = NONE;
+      } else {
+        key[win] = NONE;
+      }
+      scan();
+    }
   }
+  const double v = (int)lane < p.k ? score[my_id] : 0.0, total = p.renorm ? warp_sum(v) : 1.0;
   if ((int)lane < p.k) {
     p.ids[t * p.k + lane] = my_id;
-    p.weights[t * p.k + lane] = (float)((p.renorm ? mine / total : mine) * (double)p.scale);
+    p.weights[t * p.k + lane] = (float)(v / total * (double)p.scale);
   }
 }
 
@@ -147,12 +172,13 @@ __device__ __forceinline__ void mma_16x8x16(float (&d)[4], uint32_t a0, uint32_t
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// eight consecutive 16-bit elements of a row, `n` of which exist
+// eight consecutive 16-bit elements of a row, `n` of which exist (VEC: all or none, and no branch: loads of a batch go out together)
 template <bool VEC>
 __device__ __forceinline__ uint4 load8_raw(const uint16_t* p, int64_t n) {
   uint32_t w[4] = {0, 0, 0, 0};
   if constexpr (VEC) {
-    if (n > 0) return __ldg(reinterpret_cast<const uint4*>(p));
+    asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %5, 0;\n@p ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];\n}"
+                 : "+r"(w[0]), "+r"(w[1]), "+r"(w[2]), "+r"(w[3]) : "l"(p), "r"((uint32_t)(n > 0)));
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
@@ -162,8 +188,9 @@ __device__ __forceinline__ uint4 load8_raw(const uint16_t* p, int64_t n) {
 }
 // The warps of a CTA share its K.  The K of the operands' fragments is permuted alike, which a sum does not see: lane 4 r + c loads K 8 c .. + 7 of a
 // chunk of 32 of rows r and r + 8, one access each, and its words 0, 1 and 2, 3 are the fragments of two MMAs.
-constexpr int ROUTE_PAIR = 2;                       // tiles of sixteen experts at a time
-template <int DT, bool VEC>
+// TILES tiles of sixteen experts at a time, loads in batches of BATCH chunks.
+constexpr int ROUTE_BATCH = 4;
+template <int DT, bool VEC, int TILES>
 __global__ void __launch_bounds__(32 * ROUTE_WARPS)
 moe_route_mma_kernel(const __grid_constant__ RouteParams p)
 {
@@ -172,23 +199,24 @@ moe_route_mma_kernel(const __grid_constant__ RouteParams p)
   const uint32_t rank = ptx::cluster_ctarank();
   const int64_t t0 = (int64_t)(blockIdx.x / ROUTE_CTAS) * ROUTE_TOKENS;
   long long* key = reinterpret_cast<long long*>(s_logit + (size_t)p.splits * p.elements);
-  double* red = reinterpret_cast<double*>(key + p.elements);          // [warp][tile of the pair][16 experts][8 tokens]
+  double* red = reinterpret_cast<double*>(key + p.elements);          // [warp][tile][16 experts][8 tokens]
   const uint16_t *X = reinterpret_cast<const uint16_t*>(p.x), *W = reinterpret_cast<const uint16_t*>(p.w);
   // this CTA's tiles and K
   const int tiles = (p.E + 15) / 16, split = p.splits > 1 ? (int)rank / tiles : 0, step = p.splits > 1 ? tiles : ROUTE_CTAS;
-  const int64_t chunks = (p.H + 31) / 32, parts = (int64_t)p.splits * ROUTE_WARPS, part = (int64_t)split * ROUTE_WARPS + warp;
-  const int64_t h0 = part * chunks / parts * 32, h1 = (part + 1) * chunks / parts * 32;
+  const int chunks = (int)((p.H + 31) / 32), parts = p.splits * ROUTE_WARPS, part = split * ROUTE_WARPS + (int)warp;
+  const int c0 = (int)((int64_t)part * chunks / parts), c1 = (int)((int64_t)(part + 1) * chunks / parts);
+  cluster_arrive();
   if (tid == 0) ptx::griddep_launch_dependents();
   ptx::griddep_wait();
-  ptx::cluster_sync();                              // (all CTAs have started: their shared memory may be written)
   const bool token = t0 + r < p.T;
-  const uint16_t* x = X + (t0 + r) * p.ldx + c8;
-  for (int tile = (int)rank - split * tiles; split < p.splits && tile < tiles; tile += ROUTE_PAIR * step) {
-    const uint16_t* w[ROUTE_PAIR][2];
-    bool have[ROUTE_PAIR][2];
-    double acc[ROUTE_PAIR][4];
+  const uint16_t* x = X + (token ? t0 + r : 0) * p.ldx + c8;
+  bool waited = false;
+  for (int tile = (int)rank - split * tiles; split < p.splits && tile < tiles; tile += TILES * step) {
+    const uint16_t* w[TILES][2];
+    bool have[TILES][2];
+    double acc[TILES][4];
 #pragma unroll
-    for (int i = 0; i < ROUTE_PAIR; ++i) {
+    for (int i = 0; i < TILES; ++i) {
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const int e = (tile + i * step) * 16 + (int)r + 8 * j;
@@ -198,44 +226,54 @@ moe_route_mma_kernel(const __grid_constant__ RouteParams p)
 #pragma unroll
       for (int j = 0; j < 4; ++j) acc[i][j] = 0.0;
     }
-#pragma unroll 4
-    for (int64_t h = h0; h < h1; h += 32) {
-      const int64_t n = p.H - h - c8;
-      const uint4 b = load8_raw<VEC>(x + h, token ? n : 0);
+    for (int c = c0; c < c1; c += ROUTE_BATCH) {
+      uint4 b[ROUTE_BATCH], a[ROUTE_BATCH][TILES][2];
 #pragma unroll
-      for (int i = 0; i < ROUTE_PAIR; ++i) {
-        const uint4 lo = load8_raw<VEC>(w[i][0] + h, have[i][0] ? n : 0), hi = load8_raw<VEC>(w[i][1] + h, have[i][1] ? n : 0);
-        float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        mma_16x8x16<DT>(d, lo.x, hi.x, lo.y, hi.y, b.x, b.y);
-        mma_16x8x16<DT>(d, lo.z, hi.z, lo.w, hi.w, b.z, b.w);
+      for (int q = 0; q < ROUTE_BATCH; ++q) {
+        const int64_t h = (int64_t)(c + q) * 32, n = c + q < c1 ? p.H - h - c8 : 0;
+        b[q] = load8_raw<VEC>(x + h, token ? n : 0);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] += (double)d[j];
+        for (int i = 0; i < TILES; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) a[q][i][j] = load8_raw<VEC>(w[i][j] + h, have[i][j] ? n : 0);
       }
+#pragma unroll
+      for (int q = 0; q < ROUTE_BATCH; ++q)
+#pragma unroll
+        for (int i = 0; i < TILES; ++i) {
+          const uint4 lo = a[q][i][0], hi = a[q][i][1];
+          float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+          mma_16x8x16<DT>(d, lo.x, hi.x, lo.y, hi.y, b[q].x, b[q].y);
+          mma_16x8x16<DT>(d, lo.z, hi.z, lo.w, hi.w, b[q].z, b[q].w);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[i][j] += (double)d[j];
+        }
     }
     // accumulator j of lane 4 r + c: expert r + 8 (j / 2), token 2 c + j % 2
     __syncthreads();                                // (the sums of the tiles in front have been read)
 #pragma unroll
-    for (int i = 0; i < ROUTE_PAIR; ++i)
+    for (int i = 0; i < TILES; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) red[((warp * ROUTE_PAIR + i) * 16 + r + 8 * (j >> 1)) * 8 + 2 * (lane & 3) + (j & 1)] = acc[i][j];
+      for (int j = 0; j < 4; ++j) red[((warp * TILES + i) * 16 + r + 8 * (j >> 1)) * 8 + 2 * (lane & 3) + (j & 1)] = acc[i][j];
     __syncthreads();
-    for (int q = (int)tid; q < ROUTE_PAIR * 128; q += 32 * ROUTE_WARPS) {
+    if (!waited) { cluster_wait(); waited = true; }  // all CTAs have started: their shared memory may be written
+    for (int q = (int)tid; q < TILES * 128; q += 32 * ROUTE_WARPS) {
       const int e = (tile + (q >> 7) * step) * 16 + ((q >> 3) & 15);
       double s = 0.0;
 #pragma unroll
-      for (int v = 0; v < ROUTE_WARPS; ++v) s += red[v * ROUTE_PAIR * 128 + q];
+      for (int v = 0; v < ROUTE_WARPS; ++v) s += red[v * TILES * 128 + q];
       if (e < p.E) store_to_cta(s_logit + (size_t)split * p.elements + e, (uint32_t)q & 7u, s);
     }
   }
+  if (!waited) cluster_wait();
   ptx::cluster_sync();
   if (t0 + rank >= p.T) return;                     // token `rank` of the group is this CTA's
   if (p.splits > 1) {
     for (int e = (int)tid; e < p.E; e += 32 * ROUTE_WARPS) {
       double s = s_logit[e];
       for (int v = 1; v < p.splits; ++v) s += s_logit[(size_t)v * p.elements + e];
-      s_logit[e] = s;
+      s_logit[e] = s;                               // (choose() reads its own thread's)
     }
-    __syncthreads();
   }
   choose(p, t0 + rank, s_logit, key, red);
 }
@@ -312,13 +350,15 @@ static sdq_status_t route16(RouteParams p, bool vec, void* stream) {
   static_assert(ROUTE_TOKENS == ROUTE_CTAS);
   const int tiles = (p.E + 15) / 16;
   p.splits = tiles < ROUTE_CTAS ? ROUTE_CTAS / tiles : 1;
-  const size_t smem = ((size_t)p.splits + 1) * p.elements * 8 + (size_t)ROUTE_WARPS * ROUTE_PAIR * 128 * 8;
+  const size_t smem = ((size_t)p.splits + 1) * p.elements * 8 + (size_t)ROUTE_WARPS * (tiles > ROUTE_CTAS ? 2 : 1) * 128 * 8;
   const int64_t groups = (p.T + ROUTE_TOKENS - 1) / ROUTE_TOKENS;
-  return vec ? launch_route(moe_route_mma_kernel<DT, true>, p, groups, smem, stream) : launch_route(moe_route_mma_kernel<DT, false>, p, groups, smem, stream);
+  auto go = [&](auto kern) { return launch_route(kern, p, groups, smem, stream); };
+  if (tiles > ROUTE_CTAS) return vec ? go(moe_route_mma_kernel<DT, true, 2>) : go(moe_route_mma_kernel<DT, false, 2>);
+  return vec ? go(moe_route_mma_kernel<DT, true, 1>) : go(moe_route_mma_kernel<DT, false, 1>);
 }
 template <int G>
 static sdq_status_t route32(const RouteParams& p, bool vec, void* stream) {
-  const size_t smem = 2 * (size_t)p.elements * 8 + 2 * ROUTE_WARPS * 8;
+  const size_t smem = 2 * (size_t)p.elements * 8 + ROUTE_WARPS * 8;
   const int64_t groups = (p.T + G - 1) / G;
   return vec ? launch_route(moe_route_kernel<SDQ_FP32, G, true>, p, groups, smem, stream) : launch_route(moe_route_kernel<SDQ_FP32, G, false>, p, groups, smem, stream);
 }

@@ -27,7 +27,7 @@ def test_no_remote_shared_memory_before_the_cluster_has_started(bodies):
     assert {"mx4_linear_narrow_kernel", "mx4_linear_wide_kernel", "moe_route_kernel", "moe_route_mma_kernel", "moe_up_kernel", "moe_down_kernel"} <= set(remote)
     for n, b in remote.items():
         first, last = REMOTE.search(b).start(), [x.start() for x in REMOTE.finditer(b)][-1]
-        syncs = [x.start() for x in re.finditer(r"ptx::cluster_sync\(\)", b)]
+        syncs = [x.start() for x in re.finditer(r"ptx::cluster_sync\(\)|cluster_wait\(\)", b)]
         assert syncs[0] < first and syncs[-1] > last, n
 
 
