@@ -13,6 +13,7 @@
 
 #include "../sdq_internal.h"
 #include "layout.h"
+#include "pipe.cuh"
 #include "../sdq_ptx.cuh"
 
 namespace sdq {
@@ -28,6 +29,7 @@ struct GemmParams {
   int32_t kb;                      // records along K
   int32_t m_tiles, n_tiles;        // row tiles of 128 of both
   int32_t T;                       // narrow: token columns of a tile
+  int32_t wide_rows;               // narrow: rows of Y keep four outputs aligned
   int32_t nslot;
   int32_t pt_m, pt_n, tasks;       // wide: tiles of 256, tasks
 };
@@ -48,20 +50,23 @@ template <int DT> __device__ __forceinline__ float from_out(typename Out<DT>::ty
 }
 
 // ---- few tokens -----------------------------------------------------------------------------------------------------------
-constexpr int NARROW_THREADS = 192;                  // producer, MMA issuer, four epilogue warps
+constexpr int NARROW_THREADS = 256;                  // weights' producer, MMA issuer, tokens' producer, an idle warp, four epilogue warps
 constexpr uint32_t NARROW_TAIL = 256 + 128;          // barriers, and room to align the ring to 128 bytes
 constexpr int NARROW_MAX_SLOTS = 12;
 // slot = | weight record | codes of T tokens | scale atoms of the tokens |
 __host__ __device__ constexpr uint32_t narrow_slot(int fmt, int T) { return record(fmt) + (uint32_t)T * 128u + atoms(fmt) * ATOM; }
 
-// sum over the cluster's CTAs, in their order, of the float at `saddr`
-__device__ __forceinline__ float sum_over_cluster(uint32_t saddr, uint32_t ctas) {
-  float s = 0.0f;
-  for (uint32_t c = 0; c < ctas; ++c) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(ptx::mapa_u32(saddr, c)) : "memory");
-    s += v;
-  }
+// sum over the cluster's CTAs, in their order, of the four floats at `local`; all of them are asked for before the first is added
+__device__ __forceinline__ float4 sum_over_cluster(const float* local, uint32_t ctas) {
+  const uint32_t at = ptx::smem_u32(local);
+  float4 v[8];
+#pragma unroll
+  for (uint32_t c = 0; c < 8; ++c)
+    if (c < ctas) v[c] = ptx::ld_cluster_f32x4(ptx::mapa_u32(at, c));
+  float4 s = v[0];
+#pragma unroll
+  for (uint32_t c = 1; c < 8; ++c)
+    if (c < ctas) { s.x += v[c].x; s.y += v[c].y; s.z += v[c].z; s.w += v[c].w; }
   return s;
 }
 
@@ -91,7 +96,7 @@ mx4_linear_narrow_kernel(const __grid_constant__ GemmParams p)
   if (warp == 0) {
     if (lane == 0) {
       ptx::griddep_launch_dependents();
-      for (uint32_t i = 0; i < NSLOT; ++i) { ptx::mbar_init(&full[i], 1); ptx::mbar_init(&empty[i], 1); }
+      for (uint32_t i = 0; i < NSLOT; ++i) { ptx::mbar_init(&full[i], 2); ptx::mbar_init(&empty[i], 1); }
       ptx::mbar_init(acc_full, 1);
       ptx::fence_barrier_init();
       // the weights may be what the kernel in front writes: they are brought into L2, which holds what is written, not into
@@ -108,16 +113,21 @@ mx4_linear_narrow_kernel(const __grid_constant__ GemmParams p)
   ptx::griddep_wait();
 
   bool ok = true;
-  if (warp == 0) {
+  if (warp == 0 || warp == 2) {
     if (lane == 0) {
-      for (int i = 0; i < n_rec && ok; ++i) {
-        const uint32_t s = (uint32_t)i % NSLOT;
-        if (i >= (int)NSLOT && !(ok = ptx::mbar_wait(&empty[s], (((uint32_t)i / NSLOT) & 1u) ^ 1u))) break;
-        uint8_t* st = sm + (size_t)s * SLOT;
-        ptx::mbar_expect_tx(&full[s], SLOT);
-        ptx::bulk_g2s(st, w + (size_t)i * REC, REC, &full[s]);
-        ptx::bulk_g2s(st + REC, x + (size_t)i * REC, T * 128u, &full[s]);
-        ptx::bulk_g2s(st + REC + T * 128u, x + (size_t)i * REC + CODES, NA * ATOM, &full[s]);
+      Slot at(full, empty, sm, 1);
+      const uint8_t* src = warp ? x : w;
+      for (int i = 0; i < n_rec; ++i, src += REC) {
+        if (i >= (int)NSLOT && !(ok = wait32(at.empty, at.ph))) break;
+        if (warp == 0) {
+          expect32(at.full, REC);
+          copy32(at.at, src, REC, at.full);
+        } else {
+          expect32(at.full, T * 128u + NA * ATOM);
+          copy32(at.at + REC, src, T * 128u, at.full);
+          copy32(at.at + REC + T * 128u, src + CODES, NA * ATOM, at.full);
+        }
+        at.next(NSLOT, SLOT);
       }
       if (!ok) atomicOr(&p.flags[FLAG_TIMEOUT], 1u);
     }
@@ -127,84 +137,92 @@ mx4_linear_narrow_kernel(const __grid_constant__ GemmParams p)
       // copies to tensor memory and MMAs of one thread execute in issue order: two alternating sets of scales serve all slots
       const uint32_t id0 = ptx::idesc_block_scaled(128, T, 1, false, 0, 0) ^ (FMT == SDQ_FMT_NVFP4 ? 1u << 23 : 0u);
       const uint32_t id2 = ptx::idesc_block_scaled(128, T, 1, false, 2, 2);
-      for (int i = 0; i < n_rec && ok; ++i) {
-        const uint32_t s = (uint32_t)i % NSLOT;
-        if (!(ok = ptx::mbar_wait(&full[s], ((uint32_t)i / NSLOT) & 1u))) break;
+      Slot at(full, empty, sm, 0);
+      const uint64_t a0 = ptx::smem_desc(at.at, 128, 1024), b0 = ptx::smem_desc(at.at + REC, 128, 1024);
+      const uint64_t ca0 = ptx::smem_desc(at.at + CODES, 0, 128), cb0 = ptx::smem_desc(at.at + REC + T * 128u, 0, 128);
+      uint64_t off = 0;
+      uint32_t sfa = sets;
+      for (int i = 0; i < n_rec; ++i) {
+        if (!(ok = wait32(at.full, at.ph))) break;
         ptx::tc_fence_after();
-        const uint32_t st = ptx::smem_u32(sm) + s * SLOT, sfa = sets + (i & 1) * SET, sfb = sfa + 4 * NA;
-        const uint64_t da = ptx::smem_desc(st, 128, 1024), db = ptx::smem_desc(st + REC, 128, 1024);
-        const uint64_t ca = ptx::smem_desc(st + CODES, 0, 128), cb = ptx::smem_desc(st + REC + T * 128u, 0, 128);
+        const uint32_t sfb = sfa + 4 * NA;
 #pragma unroll
         for (uint32_t a = 0; a < NA; ++a) {
-          ptx::tc_cp_32x128b_warpx4(sfa + 4 * a, ca + a * (ATOM >> 4));
-          ptx::tc_cp_32x128b_warpx4(sfb + 4 * a, cb + a * (ATOM >> 4));
+          ptx::tc_cp_32x128b_warpx4(sfa + 4 * a, ca0 + off + a * (ATOM >> 4));
+          ptx::tc_cp_32x128b_warpx4(sfb + 4 * a, cb0 + off + a * (ATOM >> 4));
         }
 #pragma unroll
         for (uint32_t j = 0; j < 4; ++j) {                       // 64 K each: two adjacent core matrices
           const uint32_t acc = i || j ? 1u : 0u;
-          if constexpr (FMT == SDQ_FMT_NVFP4) ptx::mma_nvf4(tmem, da + ((256 * j) >> 4), db + ((256 * j) >> 4), id0, sfa + 4 * j, sfb + 4 * j, acc);
-          else ptx::mma_mxf4(tmem, da + ((256 * j) >> 4), db + ((256 * j) >> 4), j & 1 ? id2 : id0, sfa + 4 * (j >> 1), sfb + 4 * (j >> 1), acc);
+          if constexpr (FMT == SDQ_FMT_NVFP4) ptx::mma_nvf4(tmem, a0 + off + ((256 * j) >> 4), b0 + off + ((256 * j) >> 4), id0, sfa + 4 * j, sfb + 4 * j, acc);
+          else ptx::mma_mxf4(tmem, a0 + off + ((256 * j) >> 4), b0 + off + ((256 * j) >> 4), j & 1 ? id2 : id0, sfa + 4 * (j >> 1), sfb + 4 * (j >> 1), acc);
         }
-        ptx::tc_commit(&empty[s]);
+        commit32(at.empty);
+        sfa = sets + (sets + SET - sfa);                         // (the other set)
+        off += SLOT >> 4;
+        at.next(NSLOT, SLOT);
+        if (at.s == 0) off = 0;
       }
       if (ok) ptx::tc_commit(acc_full);
       else atomicOr(&p.flags[FLAG_TIMEOUT], 1u);
     }
     __syncwarp();
-  } else {
-    // warp w owns TMEM lanes 32 (w % 4) ..: weight rows
-    const uint32_t q = warp & 3, row = q * 32 + lane;
-    const int64_t n = (int64_t)nt * ROWS + row, m0 = (int64_t)mt * 128;
-    const int valid = (int)min((int64_t)T, p.M - m0);
-    float fw = 1.0f, b = 0.0f;
-    if (n < p.N) {
-      if (FMT == SDQ_FMT_NVFP4) fw = p.fw[n];
-      if (p.bias) b = from_out<DT>(reinterpret_cast<const T_out*>(p.bias)[n]);
-    }
-    T_out* y = reinterpret_cast<T_out*>(p.Y);
+  } else if (warp >= 4) {
+    // warp w moves TMEM lanes 32 (w % 4) .. (weight rows) to where the ring was: [token][128 rows]
+    const uint32_t q = warp & 3;
     ok = ptx::mbar_wait(acc_full, 0);
     if (!__all_sync(0xffffffffu, ok) && lane == 0) atomicOr(&p.flags[FLAG_TIMEOUT], 1u);
     ptx::tc_fence_after();
-    float* part = reinterpret_cast<float*>(sm) + row;            // [token][128 rows], where the ring was
-    for (int c0 = 0; c0 < valid; c0 += 16) {
-      uint32_t v[16];
-      ptx::tmem_ld_32x32b_x16(tmem + ((q * 32u) << 16) + (uint32_t)c0, v);
+    float* part = reinterpret_cast<float*>(sm) + q * 32 + lane;
+    for (uint32_t c0 = 0; c0 < T; c0 += 32) {
+      uint32_t v[2][16];
+      ptx::tmem_ld_32x32b_x16(tmem + ((q * 32u) << 16) + c0, v[0]);
+      if (c0 + 16 < T) ptx::tmem_ld_32x32b_x16(tmem + ((q * 32u) << 16) + c0 + 16, v[1]);
       ptx::tmem_ld_wait();
 #pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        if (ks > 1) part[(size_t)(c0 + j) * ROWS] = __uint_as_float(v[j]);
-        else if (c0 + j < valid && n < p.N) {
-          const float f = FMT == SDQ_FMT_NVFP4 ? fw * __ldg(p.fx + m0 + c0 + j) : 1.0f;
-          y[(m0 + c0 + j) * p.ldy + n] = to_out<DT>(fmaf(__uint_as_float(v[j]), f, b));
-        }
+      for (int j = 0; j < 16; ++j) part[(c0 + j) * ROWS] = __uint_as_float(v[0][j]);
+      if (c0 + 16 < T) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) part[(c0 + 16 + j) * ROWS] = __uint_as_float(v[1][j]);
       }
     }
     ptx::tc_fence_before();
   }
-  if (ks > 1) {
-    ptx::cluster_sync();                                         // every CTA's partial tile is in place
-    if (warp >= 2) {
-      const uint32_t row = (warp & 3) * 32 + lane;
-      const int64_t n = (int64_t)nt * ROWS + row, m0 = (int64_t)mt * 128;
-      const int valid = (int)min((int64_t)T, p.M - m0);
-      float fw = 1.0f, b = 0.0f;
-      if (n < p.N) {
-        if (FMT == SDQ_FMT_NVFP4) fw = p.fw[n];
-        if (p.bias) b = from_out<DT>(reinterpret_cast<const T_out*>(p.bias)[n]);
-      }
-      T_out* y = reinterpret_cast<T_out*>(p.Y);
-      for (int c = (int)rank; c < valid; c += (int)ks) {
-        const float s = sum_over_cluster(ptx::smem_u32(sm) + (uint32_t)(c * ROWS + (int)row) * 4u, ks);
-        if (n < p.N) {
-          const float f = FMT == SDQ_FMT_NVFP4 ? fw * __ldg(p.fx + m0 + c) : 1.0f;
-          y[(m0 + c) * p.ldy + n] = to_out<DT>(fmaf(s, f, b));
-        }
+  // every CTA's partial tile is in place
+  if (ks > 1) ptx::cluster_sync(); else __syncthreads();
+  {
+    const int64_t n0 = (int64_t)nt * ROWS, m0 = (int64_t)mt * 128;
+    const uint32_t n = (tid & 31u) * 4;                          // this thread's rows of the tile
+    float fw[4], b[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const bool in = n0 + n + j < p.N;
+      fw[j] = FMT == SDQ_FMT_NVFP4 && in ? p.fw[n0 + n + j] : 1.0f;
+      b[j] = p.bias && in ? from_out<DT>(reinterpret_cast<const T_out*>(p.bias)[n0 + n + j]) : 0.0f;
+    }
+    const int valid = (int)min((int64_t)T, p.M - m0);
+    const bool whole = n0 + n + 4 <= p.N && p.wide_rows;         // four outputs are one aligned store
+    const float* part = reinterpret_cast<const float*>(sm);
+    for (int c = (int)(rank + ks * warp); c < valid; c += (int)ks * (NARROW_THREADS / 32)) {
+      const float* src = part + c * ROWS + n;
+      const float4 s4 = ks > 1 ? sum_over_cluster(src, ks) : *reinterpret_cast<const float4*>(src);
+      const float fx = FMT == SDQ_FMT_NVFP4 ? __ldg(p.fx + m0 + c) : 1.0f;
+      const float s[4] = {s4.x, s4.y, s4.z, s4.w};
+      T_out o[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[j] = to_out<DT>(fmaf(s[j], FMT == SDQ_FMT_NVFP4 ? fw[j] * fx : 1.0f, b[j]));
+      T_out* y = reinterpret_cast<T_out*>(p.Y) + (m0 + c) * p.ldy + n0 + n;
+      if (whole) {
+        if constexpr (DT == SDQ_FP32) *reinterpret_cast<float4*>(y) = make_float4(o[0], o[1], o[2], o[3]);
+        else *reinterpret_cast<uint2*>(y) = *reinterpret_cast<const uint2*>(o);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (n0 + n + j < p.N) y[j] = o[j];
       }
     }
-    ptx::cluster_sync();                                         // nobody leaves while its partial tile is being read
-  } else {
-    __syncthreads();
   }
+  if (ks > 1) ptx::cluster_sync();                               // nobody leaves while its partial tile is being read
   if (warp == 1) ptx::tmem_dealloc(tmem, 256);
 }
 
@@ -453,8 +471,13 @@ static sdq_status_t linear(GemmParams& p, DeviceInfo* d, void* stream) {
   if (p.M <= 512) {
     p.T = p.M <= 128 ? (int32_t)(p.M + 15) / 16 * 16 : 128;
     const int64_t tiles = (int64_t)p.n_tiles * p.m_tiles;
+    // K over as many CTAs as leave the fullest SM the fewest records, two CTAs an SM at most; of equal ones the fewest
     int ks = 1;
-    while (ks < 8 && 2 * ks * tiles <= 2 * d->sm_count && 2 * ks <= p.kb) ks *= 2;
+    int64_t least = 0;
+    for (int k = 1; k <= 8 && k <= p.kb && (k == 1 || k * tiles <= 2 * d->sm_count); ++k) {
+      const int64_t most = ((k * tiles + d->sm_count - 1) / d->sm_count) * ((p.kb + k - 1) / k);
+      if (k == 1 || most < least) { ks = k; least = most; }
+    }
     const uint32_t slot = narrow_slot(FMT, p.T);
     const uint32_t room = (tiles * ks <= d->sm_count ? SMEM_MAX : SMEM_MAX / 2 - 1024) - NARROW_TAIL;
     const int want = (p.kb + ks - 1) / ks;
@@ -462,7 +485,7 @@ static sdq_status_t linear(GemmParams& p, DeviceInfo* d, void* stream) {
     if (p.nslot > want) p.nslot = want;
     if (p.nslot > NARROW_MAX_SLOTS) p.nslot = NARROW_MAX_SLOTS;
     if (p.n_tiles > 0x7FFFFFFF / 8 || p.m_tiles > 65535) return SDQ_ERR_SHAPE;
-    const uint32_t ring = (uint32_t)p.nslot * slot, parts = ks > 1 ? (uint32_t)p.T * ROWS * 4u : 0u;
+    const uint32_t ring = (uint32_t)p.nslot * slot, parts = (uint32_t)p.T * ROWS * 4u;
     // (the partial tile lies where the ring was; the barriers behind both)
     if (parts > ring) p.nslot = (int32_t)((parts + slot - 1) / slot);
     lc.gridDim = dim3((unsigned)(p.n_tiles * ks), (unsigned)p.m_tiles);
@@ -471,6 +494,7 @@ static sdq_status_t linear(GemmParams& p, DeviceInfo* d, void* stream) {
     // the columns that the other's peer waits for
     lc.dynamicSmemBytes = (uint32_t)p.nslot * slot + NARROW_TAIL > 81920u ? (uint32_t)p.nslot * slot + NARROW_TAIL : 81920u;
     attr[1].val.clusterDim.x = (unsigned)ks;
+    p.wide_rows = ((uintptr_t)p.Y % (4 * dtype_bytes(DT))) == 0 && (p.ldy % 4 == 0 || p.M == 1);
     auto kern = mx4_linear_narrow_kernel<FMT, DT>;
     if (with_smem(kern, SMEM_MAX, d, BIT) != cudaSuccess) return launch_status(cudaErrorUnknown);
     return launch_status(cudaLaunchKernelEx(&lc, kern, p));
