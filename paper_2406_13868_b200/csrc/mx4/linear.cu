@@ -227,19 +227,28 @@ mx4_linear_narrow_kernel(const __grid_constant__ GemmParams p)
 }
 
 // ---- many tokens ----------------------------------------------------------------------------------------------------------
-constexpr int WIDE_THREADS = 384;                    // producer, MMA issuer (odd CTA: forwarder), two idle, eight epilogue warps
-constexpr int WIDE_SLOTS = 5, WIDE_PAIRS = 4;
+constexpr int WIDE_THREADS = 512;                    // producer, MMA issuer, two idle, eight epilogue, four scale warps
+constexpr int WIDE_PAIRS = 4, WIDE_SETS = 4;
+// slots of the ring: what shared memory has beside the staging of outputs that are not aligned
+__host__ __device__ constexpr int wide_slots(int fmt, bool vec) { return fmt == SDQ_FMT_MXFP4 && vec ? 6 : 5; }
 // slot = | token record (codes, scale atoms) | codes of 128 weight rows | scale atoms of both CTAs' weight rows |
 __host__ __device__ constexpr uint32_t wide_slot(int fmt) { return record(fmt) + CODES + 2 * atoms(fmt) * ATOM; }
+// an arrival on a barrier of the pair's even CTA.  Relaxed: what it tells of, loads from and stores to tensor memory, has completed and been waited
+// for; a releasing arrival would wait for all of the thread's memory operations, a microsecond with a ring's copies under way
+__device__ __forceinline__ void arrive_leader(uint64_t* bar) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(ptx::mapa_u32(ptx::smem_u32(bar), 0)) : "memory");
+}
 constexpr uint32_t WIDE_PITCH = 68;                  // bytes of a staged row of 64
-constexpr uint32_t WIDE_TAIL = 256u + 2u * 2u * 256u * 4u + 8u * 32u * WIDE_PITCH + 128u;
+__host__ __device__ constexpr uint32_t wide_tail(bool vec) { return 256u + 2u * 2u * 256u * 4u + (vec ? 0u : 8u * 32u * WIDE_PITCH) + 128u; }
 
 template <int FMT, int DT, bool VEC>
 __global__ void __launch_bounds__(WIDE_THREADS)
 mx4_linear_wide_kernel(const __grid_constant__ GemmParams p)
 {
   using T_out = typename Out<DT>::type;
+  constexpr int WIDE_SLOTS = wide_slots(FMT, VEC);
   constexpr uint32_t NA = atoms(FMT), REC = record(FMT), SLOT = wide_slot(FMT), SFA_SET = 4u * NA, SET = 12u * NA;
+  static_assert(256 + WIDE_SETS * SET <= 512 && (6 + WIDE_PAIRS + 2 + WIDE_SETS) * 8 + 8 <= 256);
   constexpr uint32_t SL_B = REC, SL_SF = REC + CODES;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* sm = smem_raw + ((128 - (ptx::smem_u32(smem_raw) & 127)) & 127);
@@ -248,7 +257,8 @@ mx4_linear_wide_kernel(const __grid_constant__ GemmParams p)
   uint64_t* empty = full + WIDE_SLOTS;               // [pair of stages % WIDE_PAIRS]: the MMAs that read them have completed
   uint64_t* acc_full = empty + WIDE_PAIRS;
   uint64_t* acc_empty = acc_full + 1;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 1);
+  uint64_t* scales = acc_empty + 1;                  // [set] leader: slot landed and scales in tensor memory, in both CTAs
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(scales + WIDE_SETS);
   volatile uint32_t* timed_out = tmem_slot + 1;
   float* s_fac = reinterpret_cast<float*>(sm + WIDE_SLOTS * SLOT + 256);       // [task parity][factor, bias][256 weight rows]
   uint8_t* s_out = reinterpret_cast<uint8_t*>(s_fac + 4 * 256);
@@ -259,7 +269,8 @@ mx4_linear_wide_kernel(const __grid_constant__ GemmParams p)
 
   if (warp == 0 && lane == 0) {
     ptx::griddep_launch_dependents();
-    for (int i = 0; i < WIDE_SLOTS; ++i) ptx::mbar_init(&full[i], rank == 0 ? 2 : 1);
+    for (int i = 0; i < WIDE_SLOTS; ++i) ptx::mbar_init(&full[i], 1);
+    for (int i = 0; i < WIDE_SETS; ++i) ptx::mbar_init(&scales[i], 8);
     for (int i = 0; i < WIDE_PAIRS; ++i) ptx::mbar_init(&empty[i], 1);
     ptx::mbar_init(acc_full, 1);
     ptx::mbar_init(acc_empty, 16);
@@ -311,51 +322,73 @@ mx4_linear_wide_kernel(const __grid_constant__ GemmParams p)
       if (!ok) atomicOr(&p.flags[FLAG_TIMEOUT], 1u);
     }
     __syncwarp();
-  } else if (warp == 1 && rank == 1) {
-    if (lane == 0) {                                 // this CTA's part of a slot has landed: told to the leader
-      const int total = my_tasks * KB;
-      for (int i = 0; i < total && ok; ++i) {
-        const uint32_t s = (uint32_t)i % WIDE_SLOTS;
-        if (!(ok = ptx::mbar_wait(&full[s], ((uint32_t)i / WIDE_SLOTS) & 1u))) break;
-        ptx::mbar_arrive_remote(&full[s], 0);
-      }
-      if (!ok) atomicOr(&p.flags[FLAG_TIMEOUT], 1u);
-    }
-    __syncwarp();
   } else if (warp == 1) {
-    if (lane == 0) {
+    if (rank == 0 && lane == 0) {
       const uint32_t id0 = ptx::idesc_block_scaled(256, 256, 1, false, 0, 0) ^ (FMT == SDQ_FMT_NVFP4 ? 1u << 23 : 0u);
       const uint32_t id2 = ptx::idesc_block_scaled(256, 256, 1, false, 2, 2);
       const int total = my_tasks * KB;
+      const uint64_t a0 = ptx::smem_desc(ptx::smem_u32(sm), 128, 1024), b0 = a0 + (SL_B >> 4);
+      uint64_t off = 0;
       int i = 0;
       for (int t = 0; t < my_tasks && ok; ++t) {
         for (int k = 0; k < KB; ++k, ++i) {
-          const uint32_t s = (uint32_t)i % WIDE_SLOTS;
-          if (!(ok = ptx::mbar_wait(&full[s], ((uint32_t)i / WIDE_SLOTS) & 1u))) break;
-          if (k == 0 && t > 0 && !(ok = ptx::mbar_wait(acc_empty, (uint32_t)(t - 1) & 1u))) break;
+          if (!(ok = ptx::mbar_wait_cluster(&scales[i % WIDE_SETS], ((uint32_t)i / WIDE_SETS) & 1u))) break;
+          if (k == 0 && t > 0 && !(ok = ptx::mbar_wait_cluster(acc_empty, (uint32_t)(t - 1) & 1u))) break;
           ptx::tc_fence_after();
-          const uint32_t st = ptx::smem_u32(sm) + s * SLOT, sfa = sets + (i & 1) * SET, sfb = sfa + SFA_SET;
-          const uint64_t da = ptx::smem_desc(st, 128, 1024), db = ptx::smem_desc(st + SL_B, 128, 1024);
-          const uint64_t ca = ptx::smem_desc(st + CODES, 0, 128), cb = ptx::smem_desc(st + SL_SF, 0, 128);
-#pragma unroll
-          for (uint32_t a = 0; a < NA; ++a) {
-            ptx::tc2_cp_32x128b_warpx4(sfa + 4 * a, ca + a * (ATOM >> 4));
-            ptx::tc2_cp_32x128b_warpx4(sfb + 8 * a, cb + a * (ATOM >> 4));
-            ptx::tc2_cp_32x128b_warpx4(sfb + 8 * a + 4, cb + (NA + a) * (ATOM >> 4));
-          }
+          const uint32_t sfa = sets + (uint32_t)(i % WIDE_SETS) * SET, sfb = sfa + SFA_SET;
 #pragma unroll
           for (uint32_t j = 0; j < 4; ++j) {
             const uint32_t acc = k || j ? 1u : 0u;
-            if constexpr (FMT == SDQ_FMT_NVFP4) ptx::mma2_nvf4(tmem, da + ((256 * j) >> 4), db + ((256 * j) >> 4), id0, sfa + 4 * j, sfb + 8 * j, acc);
-            else ptx::mma2_mxf4(tmem, da + ((256 * j) >> 4), db + ((256 * j) >> 4), j & 1 ? id2 : id0, sfa + 4 * (j >> 1), sfb + 8 * (j >> 1), acc);
+            if constexpr (FMT == SDQ_FMT_NVFP4) ptx::mma2_nvf4(tmem, a0 + off + ((256 * j) >> 4), b0 + off + ((256 * j) >> 4), id0, sfa + 4 * j, sfb + 8 * j, acc);
+            else ptx::mma2_mxf4(tmem, a0 + off + ((256 * j) >> 4), b0 + off + ((256 * j) >> 4), j & 1 ? id2 : id0, sfa + 4 * (j >> 1), sfb + 8 * (j >> 1), acc);
           }
           // one release for two stages: a pair-wide commit costs the tensor pipe a bubble
           if ((i & 1) && i + 1 < total) ptx::tc2_commit_both(&empty[(uint32_t)(i >> 1) % WIDE_PAIRS], 3);
           if (k == KB - 1) ptx::tc2_commit_both(acc_full, 3);
+          off += SLOT >> 4;
+          if (off == (uint64_t)(SLOT >> 4) * WIDE_SLOTS) off = 0;
         }
       }
       if (!ok) atomicOr(&p.flags[FLAG_TIMEOUT], 1u);
     }
+    __syncwarp();
+  } else if (warp >= 12) {
+    // Scales of a slot into tensor memory, by ordinary stores of four warps (each its 32 lanes, all the same: what a copy instruction would
+    // replicate).  The copies would go through the tensor pipe, in order with its MMAs: 44 clocks each, six (MXFP4) or twelve (NVFP4) of them to
+    // four MMAs of 128 -- 850 and 1115 clocks a stage instead of 590.
+    const uint32_t q = warp & 3;
+    uint32_t s = 0;
+    const int total = my_tasks * KB;
+    for (int i = 0; i < total; ++i) {
+      ok = ptx::mbar_wait(&full[s], ((uint32_t)i / WIDE_SLOTS) & 1u);
+      if (ok && i >= WIDE_SETS) {                    // the MMAs that read this set have completed
+        const uint32_t e = (uint32_t)(i - WIDE_SETS) >> 1;
+        ok = ptx::mbar_wait(&empty[e % WIDE_PAIRS], (e / WIDE_PAIRS) & 1u);
+      }
+      if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+      const uint8_t* st = sm + (size_t)s * SLOT;
+      uint32_t v[12 * NA];                           // SFA, then of every atom the two halves of the weight rows
+#pragma unroll
+      for (uint32_t a = 0; a < NA; ++a) {
+        *reinterpret_cast<uint4*>(v + 4 * a) = *reinterpret_cast<const uint4*>(st + CODES + a * ATOM + lane * 16);
+        *reinterpret_cast<uint4*>(v + SFA_SET + 8 * a) = *reinterpret_cast<const uint4*>(st + SL_SF + a * ATOM + lane * 16);
+        *reinterpret_cast<uint4*>(v + SFA_SET + 8 * a + 4) = *reinterpret_cast<const uint4*>(st + SL_SF + (NA + a) * ATOM + lane * 16);
+      }
+      const uint32_t at = sets + (uint32_t)(i % WIDE_SETS) * SET + ((q * 32u) << 16);
+#pragma unroll
+      for (uint32_t c = 0; c + 16 <= 12 * NA; c += 16) ptx::tmem_st_32x32b_x16(at + c, *reinterpret_cast<const uint32_t(*)[16]>(v + c));
+      if constexpr (12 * NA % 16 != 0) {
+        static_assert(12 * NA % 16 == 8);
+        ptx::tmem_st_32x32b_x4(at + 12 * NA - 8, *reinterpret_cast<const uint32_t(*)[4]>(v + 12 * NA - 8));
+        ptx::tmem_st_32x32b_x4(at + 12 * NA - 4, *reinterpret_cast<const uint32_t(*)[4]>(v + 12 * NA - 4));
+      }
+      ptx::tmem_st_wait();
+      ptx::tc_fence_before();
+      __syncwarp();
+      if (lane == 0) arrive_leader(&scales[i % WIDE_SETS]);
+      if (++s == WIDE_SLOTS) s = 0;
+    }
+    if (!ok && lane == 0) atomicOr(&p.flags[FLAG_TIMEOUT], 1u);
     __syncwarp();
   } else if (warp >= 4) {
     // epilogue: warp w owns TMEM lanes 32 (w % 4) .. (tokens); warps 4 to 7 the first 128 weight rows, 8 to 11 the others.  The
@@ -377,61 +410,69 @@ mx4_linear_wide_kernel(const __grid_constant__ GemmParams p)
       ptx::named_bar_sync(1, 256);
       if (*timed_out) { ok = false; break; }
       ptx::tc_fence_after();
-      constexpr int PER = DT == SDQ_FP32 ? 1 : 2, WORDS = 128 / PER;
-      uint32_t out[WORDS];
+      // (four-byte outputs in two parts: what a thread holds is 64 words)
+      constexpr int PER = DT == SDQ_FP32 ? 1 : 2, WORDS = 64, COLS = WORDS * PER, PARTS = 128 / COLS;
+      const bool stored = 2 * mt + (int)rank < p.m_tiles;        // (not the repeated last tile)
+#pragma unroll 1
+      for (int part = 0; part < PARTS; ++part) {
+        const uint32_t c0 = half * 128u + (uint32_t)(part * COLS);
+        uint32_t out[WORDS];
 #pragma unroll
-      for (int c = 0; c < 8; ++c) {
-        uint32_t v[16];
-        ptx::tmem_ld_32x32b_x16(tmem + ((q * 32u) << 16) + half * 128u + 16u * c, v);
-        ptx::tmem_ld_wait();
+        for (int c = 0; c < COLS / 16; ++c) {
+          uint32_t v[16];
+          ptx::tmem_ld_32x32b_x16(tmem + ((q * 32u) << 16) + c0 + 16u * c, v);
+          ptx::tmem_ld_wait();
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          const uint32_t col = half * 128u + 16u * c + j;
-          v[j] = __float_as_uint(fmaf(__uint_as_float(v[j]), FMT == SDQ_FMT_NVFP4 ? fac[col] * fx : 1.0f, fac[256 + col]));
-        }
+          for (int j = 0; j < 16; ++j) {
+            const uint32_t col = c0 + 16u * c + j;
+            v[j] = __float_as_uint(fmaf(__uint_as_float(v[j]), FMT == SDQ_FMT_NVFP4 ? fac[col] * fx : 1.0f, fac[256 + col]));
+          }
 #pragma unroll
-        for (int j = 0; j < 16 / PER; ++j) {
-          if constexpr (DT == SDQ_FP32) out[16 * c + j] = v[j];
-          else if constexpr (DT == SDQ_BF16) {
-            const __nv_bfloat162 b = __floats2bfloat162_rn(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]));
-            out[8 * c + j] = *reinterpret_cast<const uint32_t*>(&b);
-          } else {
-            const __half2 b = __floats2half2_rn(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]));
-            out[8 * c + j] = *reinterpret_cast<const uint32_t*>(&b);
+          for (int j = 0; j < 16 / PER; ++j) {
+            if constexpr (DT == SDQ_FP32) out[16 * c + j] = v[j];
+            else if constexpr (DT == SDQ_BF16) {
+              const __nv_bfloat162 b = __floats2bfloat162_rn(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]));
+              out[8 * c + j] = *reinterpret_cast<const uint32_t*>(&b);
+            } else {
+              const __half2 b = __floats2half2_rn(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]));
+              out[8 * c + j] = *reinterpret_cast<const uint32_t*>(&b);
+            }
           }
         }
-      }
-      ptx::tc_fence_before();
-      __syncwarp();
-      if (lane == 0) { if (rank == 0) ptx::mbar_arrive(acc_empty); else ptx::mbar_arrive_remote(acc_empty, 0); }
-      if (2 * mt + (int)rank >= p.m_tiles) continue;             // (the repeated last tile)
-      T_out* y = reinterpret_cast<T_out*>(p.Y) + m * p.ldy + n0 + half * 128;
-      const int cols = (int)min((int64_t)128, p.N - n0 - (int64_t)half * 128);
-      if constexpr (VEC) {
-        if (m < p.M) {
-#pragma unroll
-          for (int c = 0; c < WORDS / 8; ++c) {                  // 32 bytes, one sector, a store
-            constexpr int EL = 8 * PER;
-            if ((c + 1) * EL <= cols)
-              asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(y + c * EL), "r"(out[8 * c]), "r"(out[8 * c + 1]), "r"(out[8 * c + 2]),
-                           "r"(out[8 * c + 3]), "r"(out[8 * c + 4]), "r"(out[8 * c + 5]), "r"(out[8 * c + 6]), "r"(out[8 * c + 7]) : "memory");
-          }
+        if (part == PARTS - 1) {                                 // the accumulator has been read
+          ptx::tc_fence_before();
+          __syncwarp();
+          if (lane == 0) arrive_leader(acc_empty);
         }
-      } else {
-        // any alignment: 64 bytes of 32 tokens at a time turned in shared memory, consecutive lanes store consecutive outputs of a token
-        constexpr int EL = 16 * PER, RUN = 32 / EL;              // outputs of a token at a time, tokens a store instruction covers
-        uint8_t* st = s_out + (warp - 4) * 32u * WIDE_PITCH;
-        const int64_t mw = m - lane;
-        const int rows = (int)min((int64_t)32, p.M - mw), col = (int)lane % EL, r0 = (int)lane / EL;
+        if (!stored) continue;
+        T_out* y = reinterpret_cast<T_out*>(p.Y) + m * p.ldy + n0 + c0;
+        const int cols = (int)min((int64_t)COLS, p.N - n0 - (int64_t)c0);
+        if constexpr (VEC) {
+          if (m < p.M) {
 #pragma unroll
-        for (int c = 0; c < WORDS / 16; ++c) {
-          __syncwarp();
+            for (int c = 0; c < WORDS / 8; ++c) {                // 32 bytes, one sector, a store
+              constexpr int EL = 8 * PER;
+              if ((c + 1) * EL <= cols)
+                asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(y + c * EL), "r"(out[8 * c]), "r"(out[8 * c + 1]), "r"(out[8 * c + 2]),
+                             "r"(out[8 * c + 3]), "r"(out[8 * c + 4]), "r"(out[8 * c + 5]), "r"(out[8 * c + 6]), "r"(out[8 * c + 7]) : "memory");
+            }
+          }
+        } else {
+          // any alignment: 64 bytes of 32 tokens at a time turned in shared memory, consecutive lanes store consecutive outputs of a token
+          constexpr int EL = 16 * PER, RUN = 32 / EL;            // outputs of a token at a time, tokens a store instruction covers
+          uint8_t* st = s_out + (warp - 4) * 32u * WIDE_PITCH;
+          const int64_t mw = m - lane;
+          const int rows = (int)min((int64_t)32, p.M - mw), col = (int)lane % EL, r0 = (int)lane / EL;
 #pragma unroll
-          for (int j = 0; j < 16; ++j) *reinterpret_cast<uint32_t*>(st + lane * WIDE_PITCH + 4u * j) = out[16 * c + j];
-          __syncwarp();
-          if (c * EL + col < cols) {
-            T_out* yr = reinterpret_cast<T_out*>(p.Y) + mw * p.ldy + n0 + half * 128 + c * EL + col;
-            for (int r = r0; r < rows; r += RUN) yr[(int64_t)r * p.ldy] = *reinterpret_cast<const T_out*>(st + r * WIDE_PITCH + col * sizeof(T_out));
+          for (int c = 0; c < WORDS / 16; ++c) {
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < 16; ++j) *reinterpret_cast<uint32_t*>(st + lane * WIDE_PITCH + 4u * j) = out[16 * c + j];
+            __syncwarp();
+            if (c * EL + col < cols) {
+              T_out* yr = reinterpret_cast<T_out*>(p.Y) + mw * p.ldy + n0 + c0 + c * EL + col;
+              for (int r = r0; r < rows; r += RUN) yr[(int64_t)r * p.ldy] = *reinterpret_cast<const T_out*>(st + r * WIDE_PITCH + col * sizeof(T_out));
+            }
           }
         }
       }
@@ -506,16 +547,18 @@ static sdq_status_t linear(GemmParams& p, DeviceInfo* d, void* stream) {
   const int pairs = d->sm_count / 2 < p.tasks ? d->sm_count / 2 : p.tasks;
   lc.gridDim = dim3(2 * (unsigned)pairs);
   lc.blockDim = dim3(WIDE_THREADS);
-  lc.dynamicSmemBytes = WIDE_SLOTS * wide_slot(FMT) + WIDE_TAIL;
-  static_assert(WIDE_SLOTS * wide_slot(FMT) + WIDE_TAIL <= SMEM_MAX, "the ring fits");
   attr[1].val.clusterDim.x = 2;
   const int64_t sector = 32 / (int64_t)dtype_bytes(DT);
   const bool vec = ((uintptr_t)p.Y & 31) == 0 && p.ldy % sector == 0 && p.N % sector == 0;
-  auto go = [&](auto kern, int bit) {
-    if (with_smem(kern, lc.dynamicSmemBytes, d, bit) != cudaSuccess) return launch_status(cudaErrorUnknown);
+  auto go = [&](auto kern, auto v, int bit) {
+    constexpr bool V = decltype(v)::value;
+    constexpr uint32_t bytes = wide_slots(FMT, V) * wide_slot(FMT) + wide_tail(V);
+    static_assert(bytes <= SMEM_MAX, "the ring fits");
+    lc.dynamicSmemBytes = bytes;
+    if (with_smem(kern, bytes, d, bit) != cudaSuccess) return launch_status(cudaErrorUnknown);
     return launch_status(cudaLaunchKernelEx(&lc, kern, p));
   };
-  return vec ? go(mx4_linear_wide_kernel<FMT, DT, true>, BIT + 1) : go(mx4_linear_wide_kernel<FMT, DT, false>, BIT + 2);
+  return vec ? go(mx4_linear_wide_kernel<FMT, DT, true>, std::true_type{}, BIT + 1) : go(mx4_linear_wide_kernel<FMT, DT, false>, std::false_type{}, BIT + 2);
 }
 
 }  // namespace mx4

@@ -9,6 +9,7 @@
 #include "../sdq_codec.cuh"
 #include "../sdq_internal.h"
 #include "layout.h"
+#include "pipe.cuh"
 #include "../sdq_ptx.cuh"
 
 namespace sdq {
@@ -207,9 +208,18 @@ __device__ __forceinline__ float keep_side(float z, float a, float b) {
   }
   return z;
 }
-// E4M3 code nearest to a / 6 (a >= 0, at most 2688), at least the smallest positive one unless the block is all zero
+// a / b with r = 1 / b to within a few units: the quotient's estimate, its exact remainder, one correction (Markstein).  An exact quotient of
+// few bits comes out as itself, so that ties stay ties.  (The remainder is taken as q b - a, so that a negative zero stays one.)
+__device__ __forceinline__ float quotient(float a, float b, float r) {
+  const float q = a * r;
+  return fmaf(-fmaf(q, b, -a), r, q);
+}
+// E4M3 code nearest to a / 6 (a >= 0, at most 2688), at least the smallest positive one unless the block is all zero.  Only an fp32 a
+// can have a quotient so near to a boundary that rounding puts it there
+template <int DT>
 __device__ __forceinline__ uint32_t nv_scale_code(float a, bool nonzero) {
-  const uint32_t c = e4m3x1(keep_side<19>(__fdiv_rn(a, 6.0f), a, 6.0f));
+  const float z = quotient(a, 6.0f, 1.0f / 6.0f);
+  const uint32_t c = e4m3x1(DT == SDQ_FP32 ? keep_side<19>(z, a, 6.0f) : z);
   return nonzero ? max(c, 1u) : 0u;
 }
 __device__ __forceinline__ float e4m3_value(uint32_t c) { return __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)c, __NV_E4M3))); }
@@ -244,20 +254,35 @@ __device__ __forceinline__ uint2 encode_mx(float (&v)[16], bool ceil_rule, uint3
   scale = a != a ? 255u : c;
   return codes16(v);
 }
-// NVFP4: a block; `down` = 2^-t of the row
+// NVFP4: the row's factor 2^t, as what its elements are worked on with.  Rows of tiny numbers are lifted by 2^64 first, which keeps
+// remainders out of the subnormal range
+struct NvRow {
+  float lift, down, up;                      // 2^0 or 2^64; 2^-t, 2^t of the lifted row
+  __device__ __forceinline__ explicit NvRow(int t) {
+    const bool tiny = t < -60;
+    lift = tiny ? 18446744073709551616.0f : 1.0f;
+    down = pow2_neg(tiny ? t + 64 : t);
+    up = pow2_neg(tiny ? -t - 64 : -t);
+  }
+};
+// a block
 template <int DT>
-__device__ __forceinline__ uint2 encode_nv(float (&v)[16], float down, uint32_t& scale) {
+__device__ __forceinline__ uint2 encode_nv(float (&v)[16], const NvRow& row, uint32_t& scale) {
+  if (row.lift != 1.0f) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] *= row.lift;
+  }
   float a = max16(v);
   saturate<DT>(v, a);
-  scale = a != a ? 127u : nv_scale_code(a * down, a > 0.0f);
-  const float s = e4m3_value(scale), r = scale ? __frcp_rn(s) : 0.0f;
+  scale = a != a ? 127u : nv_scale_code<DT>(a * row.down, a > 0.0f);
+  const float s = e4m3_value(scale) * row.up;
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
+  if (scale == 0u) r = 0.0f;
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    // y / s correctly rounded (Markstein: quotient estimate, its exact remainder, one correction): ties stay ties
-    const float y = v[i] * down, q = y * r;
-    // (the remainder taken as q s - y, so that a negative zero stays one)
-    const float z = fmaf(-fmaf(q, s, -y), r, q);
-    v[i] = DT == SDQ_FP32 ? keep_side<21>(z, y, s) : z;
+    const float z = quotient(v[i], s, r);
+    v[i] = DT == SDQ_FP32 ? keep_side<21>(z, v[i], s) : z;
   }
   return codes16(v);
 }
@@ -411,14 +436,14 @@ nv4_quantize_kernel(const typename Elem<DT>::type* __restrict__ X, Shape s, uint
   }
   a = max_over_cluster(mx, a, warp, lane, warps, ctas, rank);
   const int t = nv_row_exp(fminf(a, type_max<DT>()));
-  const float down = pow2_neg(t);
+  const NvRow nv(t);
   if (rank == 0 && warp == 0 && (lane & 3) == 0 && r >= 0) *reinterpret_cast<float*>(buf + s.factors + (size_t)r * 4) = __uint_as_float((uint32_t)(t + 127) << 23);
   auto encode = [&](float (&w)[2][16], int64_t u) {
     const Unit x = unit_at<false, SDQ_FMT_NVFP4>(buf, g, u, s.kblocks, lane);
     uint32_t sc[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const uint2 c = encode_nv<DT>(w[h], down, sc[h]);
+      const uint2 c = encode_nv<DT>(w[h], nv, sc[h]);
       if (r >= 0) put_codes(x, h, c);
     }
     put_scales<SDQ_FMT_NVFP4>(x, sc, lane, r >= 0);
@@ -435,6 +460,96 @@ nv4_quantize_kernel(const typename Elem<DT>::type* __restrict__ X, Shape s, uint
       const int64_t u = (int64_t)(rank + ctas * (warp + warps * n));
       if (u < s.units) encode(v[n], u);
     }
+  }
+}
+
+// Many rows: one CTA an SM goes through them RB at a time, the next ones on their way into shared memory (bulk copies) while these are read
+// there twice, for the maxima and to be encoded.  A row is read from DRAM once and nothing waits for anybody else (8192 x 11008 bf16: the
+// cluster form, a barrier and a half between a row's load and its codes, 110 us; reading rows again from L2 82).
+constexpr int NS_WARPS = 16, NS_MAX_BUFFERS = 8;
+template <int DT, int RB>
+__global__ void __launch_bounds__(32 * NS_WARPS)
+nv4_quantize_stream_kernel(const typename Elem<DT>::type* __restrict__ X, Shape s, int buffers, uint32_t row_bytes, uint8_t* __restrict__ buf, uint32_t* __restrict__ flags)
+{
+  using T = typename Elem<DT>::type;
+  constexpr int LPR = 32 / RB, RUN = 16 * LPR;               // lanes of a row, elements of it that a warp takes at a time
+  extern __shared__ __align__(16) uint8_t ring[];            // [buffer][RB][row_bytes]
+  __shared__ uint64_t full[NS_MAX_BUFFERS];
+  __shared__ float s_max[2][NS_WARPS][RB];
+  const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, rl = lane / LPR, kl = (lane % LPR) * 16;
+  const int64_t blocks = (s.R + RB - 1) / RB;
+  auto load = [&](int64_t b, int n) {                        // (one thread)
+    const int rows = (int)min((int64_t)RB, s.R - b * RB);
+    const uint32_t bar = ptx::smem_u32(&full[n]), dst = ptx::smem_u32(ring) + (uint32_t)n * RB * row_bytes;
+    expect32(bar, (uint32_t)rows * (uint32_t)s.K * (uint32_t)sizeof(T));
+    for (int r = 0; r < rows; ++r) copy32(dst + (uint32_t)r * row_bytes, X + (b * RB + r) * s.ld, (uint32_t)s.K * (uint32_t)sizeof(T), bar);
+  };
+  if (tid == 0) {
+    for (int n = 0; n < buffers; ++n) ptx::mbar_init(&full[n], 1);
+    ptx::fence_barrier_init();
+    ptx::griddep_launch_dependents();
+  }
+  __syncthreads();
+  ptx::griddep_wait();
+  if (tid == 0)
+    for (int n = 0; n < buffers; ++n)
+      if (blockIdx.x + (int64_t)n * gridDim.x < blocks) load(blockIdx.x + (int64_t)n * gridDim.x, n);
+  int n = 0, turn = 0;
+  uint32_t ph = 0;
+  for (int64_t b = blockIdx.x; b < blocks; b += gridDim.x, turn ^= 1) {
+    if (!wait32(ptx::smem_u32(&full[n]), ph)) { if (lane == 0) atomicOr(&flags[FLAG_TIMEOUT], 1u); return; }
+    const uint8_t* row = ring + ((uint32_t)n * RB + rl) * row_bytes;
+    const int64_t r = b * RB + rl;
+    const bool have = r < s.R;
+    auto read = [&](float (&v)[16], int64_t k) {             // (K is a multiple of a granule's elements)
+      constexpr int PER = 16 / sizeof(T);
+#pragma unroll
+      for (int i = 0; i < 16 / PER; ++i) {
+        uint4 q = make_uint4(0, 0, 0, 0);
+        if (have && k + i * PER < s.K) q = *reinterpret_cast<const uint4*>(row + (size_t)(k + i * PER) * sizeof(T));
+        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if constexpr (DT == SDQ_FP32) v[4 * i + j] = __uint_as_float(w[j]);
+          else if constexpr (DT == SDQ_BF16) { v[8 * i + 2 * j] = __uint_as_float(w[j] << 16); v[8 * i + 2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u); }
+          else { const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[j])); v[8 * i + 2 * j] = f.x; v[8 * i + 2 * j + 1] = f.y; }
+        }
+      }
+    };
+    float a = 0.0f, v[16];
+    for (int64_t k = (int64_t)warp * RUN + kl; k < s.K; k += NS_WARPS * RUN) {
+      read(v, k);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) a = fmaxf(a, fabsf(v[i]));
+    }
+#pragma unroll
+    for (int o = 1; o < LPR; o <<= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
+    if (lane % LPR == 0) s_max[turn][warp][rl] = a;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < NS_WARPS; ++w) a = fmaxf(a, s_max[turn][w][rl]);
+    const int t = nv_row_exp(fminf(a, type_max<DT>()));
+    const NvRow nv(t);
+    if (warp == 0 && lane % LPR == 0 && have) *reinterpret_cast<float*>(buf + s.factors + (size_t)r * 4) = __uint_as_float((uint32_t)(t + 127) << 23);
+    uint8_t* tile = buf + (size_t)(r / ROWS) * s.kblocks * record(SDQ_FMT_NVFP4);
+    const uint32_t rr = (uint32_t)(r % ROWS);
+    for (int64_t k = (int64_t)warp * RUN + kl; k < s.units * UNIT_K; k += NS_WARPS * RUN) {      // (padding included)
+      read(v, k);
+      uint32_t sc;
+      const uint2 c = encode_nv<DT>(v, nv, sc);
+      uint32_t w = sc << (8 * (lane & 3));
+      w |= __shfl_xor_sync(0xffffffffu, w, 1);
+      w |= __shfl_xor_sync(0xffffffffu, w, 2);
+      if (have) {
+        uint8_t* rec = tile + (size_t)(k / KREC) * record(SDQ_FMT_NVFP4);
+        const uint32_t kk = (uint32_t)(k % KREC);
+        *reinterpret_cast<uint2*>(rec + (rr >> 3) * 1024 + (kk >> 5) * 128 + (rr & 7) * 16 + (kk >> 1 & 8)) = c;
+        if ((lane & 3) == 0) *reinterpret_cast<uint32_t*>(rec + CODES + (kk >> 6) * ATOM + atom_off(rr, 0)) = w;
+      }
+    }
+    __syncthreads();                                         // the buffer has been read
+    if (tid == 0 && b + (int64_t)buffers * gridDim.x < blocks) load(b + (int64_t)buffers * gridDim.x, n);
+    if (++n == buffers) { n = 0; ph ^= 1u; }
   }
 }
 
@@ -571,10 +686,12 @@ static Shape shape_of(int64_t E, int64_t R, int64_t K, int64_t ld, int fmt) {
   return s;
 }
 template <typename... P, typename... A>
-static sdq_status_t launch_cluster(unsigned cluster, void (*kern)(P...), dim3 grid, unsigned threads, void* stream, A... args) {
+static sdq_status_t launch_as(unsigned cluster, size_t smem, void (*kern)(P...), dim3 grid, unsigned threads, void* stream, A... args) {
+
   cudaLaunchConfig_t lc = {};
   lc.gridDim = grid;
   lc.blockDim = dim3(threads);
+  lc.dynamicSmemBytes = smem;
   lc.stream = (cudaStream_t)stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -588,7 +705,9 @@ static sdq_status_t launch_cluster(unsigned cluster, void (*kern)(P...), dim3 gr
   return launch_status(cudaLaunchKernelEx(&lc, kern, args...));
 }
 template <typename... P, typename... A>
-static sdq_status_t launch(void (*kern)(P...), dim3 grid, unsigned threads, void* stream, A... args) { return launch_cluster(0, kern, grid, threads, stream, args...); }
+static sdq_status_t launch(void (*kern)(P...), dim3 grid, unsigned threads, void* stream, A... args) { return launch_as(0, 0, kern, grid, threads, stream, args...); }
+constexpr int NS_SMEM = 227328;              // (beside the kernel's own)
+constexpr int64_t NS_FROM = 1 << 22;          // elements from which rows are streamed
 // 8-row groups, one a thread block along x: linear: those that hold rows; experts: of all padded rows
 static int64_t groups_of(int64_t E, const Shape& s) { return E ? E * s.tiles * 16 : (s.R + 7) / 8; }
 static unsigned blocks_along_k(const Shape& s, int warps) { return (unsigned)((s.units + warps - 1) / warps < 65535 ? (s.units + warps - 1) / warps : 65535); }
@@ -610,12 +729,33 @@ static sdq_status_t quantize(const void* X, int64_t E, const Shape& s, int fmt, 
   const int64_t groups = groups_of(E, s);
   if (groups > 0x7FFFFFFF) return SDQ_ERR_SHAPE;
   if (fmt == SDQ_FMT_NVFP4) {
+    // rows in 16-byte granules, enough of them to go round the SMs at least twice, and two or more buffers of them
+    const uint32_t row_bytes = (uint32_t)((s.K * (int64_t)sizeof(T) + 15) / 16 * 16);
+    const int64_t per = 16 / (int64_t)sizeof(T);
+    DeviceInfo* d = device_info();
+    uint32_t* flags = device_flags();
+    if (!d || !flags) return SDQ_ERR_CUDA;
+    if (((uintptr_t)X & 15) == 0 && s.K % per == 0 && s.ld % per == 0 && s.K * (int64_t)sizeof(T) <= 49152 && s.K * (int64_t)sizeof(T) >= 4096 && s.R * s.K >= NS_FROM) {
+      auto stream_rows = [&](auto kern, int rb, int bit) {
+        if (!(d->mx4_quant_attr & (1u << bit))) {
+          if (cudaFuncSetAttribute((const void*)kern, cudaFuncAttributeMaxDynamicSharedMemorySize, NS_SMEM) != cudaSuccess) return launch_status(cudaErrorUnknown);
+          d->mx4_quant_attr |= 1u << bit;
+        }
+        int buffers = NS_SMEM / (int)(row_bytes * (uint32_t)rb);
+        if (buffers > NS_MAX_BUFFERS) buffers = NS_MAX_BUFFERS;
+        const int64_t blocks = (s.R + rb - 1) / rb;
+        return launch_as(0, (size_t)buffers * rb * row_bytes, kern, dim3((unsigned)(blocks < d->sm_count ? blocks : d->sm_count)), 32 * NS_WARPS, stream, x, s, buffers, row_bytes, buf, flags);
+      };
+      if (row_bytes * 16u <= NS_SMEM) return stream_rows(nv4_quantize_stream_kernel<DT, 8>, 8, 3 * DT);
+      if (row_bytes * 8u <= NS_SMEM) return stream_rows(nv4_quantize_stream_kernel<DT, 4>, 4, 3 * DT + 1);
+      return stream_rows(nv4_quantize_stream_kernel<DT, 2>, 2, 3 * DT + 2);
+    }
     // one unit a warp where the CTAs of a cluster have as many warps, else two; short rows take fewer warps
     const int nu = s.units <= NV_CTAS * Q_WARPS ? 1 : 2;
     const int64_t warps = (s.units + nu - 1) / nu, ctas = (warps + Q_WARPS - 1) / Q_WARPS;
     if (ctas > NV_CTAS) return vec ? launch(nv4_quantize_kernel<DT, true, 1, true>, dim3((unsigned)groups), 32 * Q_WARPS, stream, x, s, buf)
                                    : launch(nv4_quantize_kernel<DT, false, 1, true>, dim3((unsigned)groups), 32 * Q_WARPS, stream, x, s, buf);
-    auto nv = [&](auto kern) { return launch_cluster((unsigned)ctas, kern, dim3((unsigned)groups, (unsigned)ctas), 32u * (unsigned)((warps + ctas - 1) / ctas), stream, x, s, buf); };
+    auto nv = [&](auto kern) { return launch_as((unsigned)ctas, 0, kern, dim3((unsigned)groups, (unsigned)ctas), 32u * (unsigned)((warps + ctas - 1) / ctas), stream, x, s, buf); };
     if (nu == 1) return vec ? nv(nv4_quantize_kernel<DT, true, 1, false>) : nv(nv4_quantize_kernel<DT, false, 1, false>);
     return vec ? nv(nv4_quantize_kernel<DT, true, 2, false>) : nv(nv4_quantize_kernel<DT, false, 2, false>);
   }

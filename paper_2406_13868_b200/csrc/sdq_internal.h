@@ -25,6 +25,7 @@ struct DeviceInfo {
   std::atomic<uint32_t> diag_attr;      // the copy-rate diagnostic
   std::atomic<uint32_t> group_attr;     // the grouped few-token GEMM
   std::atomic<uint32_t> mx4_attr;       // bit per instantiation of the microscaled 4-bit GEMMs
+  std::atomic<uint32_t> mx4_quant_attr; // bit per instantiation of the row-streaming quantizer
   std::atomic<uint32_t> moe_attr;       // the expert layer's kernels
   std::atomic<uint32_t> clusters_known; // 1: pair_clusters is filled in
   int pair_clusters[5];    // CTA-pair GEMM: clusters of k pairs that run at once
