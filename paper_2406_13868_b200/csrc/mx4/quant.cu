@@ -6,6 +6,8 @@
 // Bound by DRAM traffic: 2 to 4 bytes an element on one side, 0.53 or 0.56 on the other.
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "../sdq_codec.cuh"
 #include "../sdq_internal.h"
 #include "layout.h"
@@ -463,9 +465,11 @@ nv4_quantize_kernel(const typename Elem<DT>::type* __restrict__ X, Shape s, uint
   }
 }
 
-// Many rows: one CTA an SM goes through them RB at a time, the next ones on their way into shared memory (bulk copies) while these are read
-// there twice, for the maxima and to be encoded.  A row is read from DRAM once and nothing waits for anybody else (8192 x 11008 bf16: the
-// cluster form, a barrier and a half between a row's load and its codes, 110 us; reading rows again from L2 82).
+// Many long rows of a 16-bit type: one CTA an SM goes through them RB at a time, the next ones on their way into shared memory (bulk copies)
+// while these are read there twice, for the maxima and to be encoded.  A row is read from DRAM once and nothing waits for anybody else.
+// us, this and the cluster form: 8192 x 11008 bf16 67 and 99 (rows read again from L2: 82), 4096 x 16384 53 and 71, 512 x 11008 7.8 and 9.8; but 300 x
+// 11008 6.1 and 4.7, and where a warp of the cluster form has one unit, 2048 x 4096 10.9 and 9.4, 8192 x 4096 29.0 and 28.5.  Issue slots 56 %
+// taken, DRAM 54 %: the two passes and the barriers between them are what is left.
 constexpr int NS_WARPS = 16, NS_MAX_BUFFERS = 8;
 template <int DT, int RB>
 __global__ void __launch_bounds__(32 * NS_WARPS)
@@ -510,17 +514,30 @@ nv4_quantize_stream_kernel(const typename Elem<DT>::type* __restrict__ X, Shape 
         const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          if constexpr (DT == SDQ_FP32) v[4 * i + j] = __uint_as_float(w[j]);
-          else if constexpr (DT == SDQ_BF16) { v[8 * i + 2 * j] = __uint_as_float(w[j] << 16); v[8 * i + 2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u); }
+          static_assert(DT != SDQ_FP32);
+          if constexpr (DT == SDQ_BF16) { v[8 * i + 2 * j] = __uint_as_float(w[j] << 16); v[8 * i + 2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u); }
           else { const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[j])); v[8 * i + 2 * j] = f.x; v[8 * i + 2 * j + 1] = f.y; }
         }
       }
     };
     float a = 0.0f, v[16];
-    for (int64_t k = (int64_t)warp * RUN + kl; k < s.K; k += NS_WARPS * RUN) {
-      read(v, k);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) a = fmaxf(a, fabsf(v[i]));
+    {
+      using T2 = typename std::conditional<DT == SDQ_BF16, __nv_bfloat162, __half2>::type;
+      auto larger = [](uint32_t m, uint32_t x) {
+        x &= 0x7FFF7FFFu;
+        const T2 r = __hmax2(*reinterpret_cast<const T2*>(&m), *reinterpret_cast<const T2*>(&x));
+        return *reinterpret_cast<const uint32_t*>(&r);
+      };
+      uint32_t m0 = 0, m1 = 0;
+      const int granules = have ? (int)s.K / 8 : 0;
+#pragma unroll 4
+      for (int k = (int)(warp * LPR + lane % LPR); k < granules; k += NS_WARPS * LPR) {
+        const uint4 q = reinterpret_cast<const uint4*>(row)[k];
+        m0 = larger(m0, q.x); m1 = larger(m1, q.y); m0 = larger(m0, q.z); m1 = larger(m1, q.w);
+      }
+      m0 = larger(m0, m1);
+      if constexpr (DT == SDQ_BF16) a = fmaxf(__uint_as_float(m0 << 16), __uint_as_float(m0 & 0xFFFF0000u));
+      else { const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&m0)); a = fmaxf(f.x, f.y); }
     }
 #pragma unroll
     for (int o = 1; o < LPR; o <<= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
@@ -729,26 +746,28 @@ static sdq_status_t quantize(const void* X, int64_t E, const Shape& s, int fmt, 
   const int64_t groups = groups_of(E, s);
   if (groups > 0x7FFFFFFF) return SDQ_ERR_SHAPE;
   if (fmt == SDQ_FMT_NVFP4) {
-    // rows in 16-byte granules, enough of them to go round the SMs at least twice, and two or more buffers of them
+    // rows in 16-byte granules, more than one unit a warp in the cluster form, 2^22 elements of them at least, and two buffers that fit
     const uint32_t row_bytes = (uint32_t)((s.K * (int64_t)sizeof(T) + 15) / 16 * 16);
     const int64_t per = 16 / (int64_t)sizeof(T);
     DeviceInfo* d = device_info();
     uint32_t* flags = device_flags();
     if (!d || !flags) return SDQ_ERR_CUDA;
-    if (((uintptr_t)X & 15) == 0 && s.K % per == 0 && s.ld % per == 0 && s.K * (int64_t)sizeof(T) <= 49152 && s.K * (int64_t)sizeof(T) >= 4096 && s.R * s.K >= NS_FROM) {
-      auto stream_rows = [&](auto kern, int rb, int bit) {
-        if (!(d->mx4_quant_attr & (1u << bit))) {
-          if (cudaFuncSetAttribute((const void*)kern, cudaFuncAttributeMaxDynamicSharedMemorySize, NS_SMEM) != cudaSuccess) return launch_status(cudaErrorUnknown);
-          d->mx4_quant_attr |= 1u << bit;
-        }
-        int buffers = NS_SMEM / (int)(row_bytes * (uint32_t)rb);
-        if (buffers > NS_MAX_BUFFERS) buffers = NS_MAX_BUFFERS;
-        const int64_t blocks = (s.R + rb - 1) / rb;
-        return launch_as(0, (size_t)buffers * rb * row_bytes, kern, dim3((unsigned)(blocks < d->sm_count ? blocks : d->sm_count)), 32 * NS_WARPS, stream, x, s, buffers, row_bytes, buf, flags);
-      };
-      if (row_bytes * 16u <= NS_SMEM) return stream_rows(nv4_quantize_stream_kernel<DT, 8>, 8, 3 * DT);
-      if (row_bytes * 8u <= NS_SMEM) return stream_rows(nv4_quantize_stream_kernel<DT, 4>, 4, 3 * DT + 1);
-      return stream_rows(nv4_quantize_stream_kernel<DT, 2>, 2, 3 * DT + 2);
+    if constexpr (DT != SDQ_FP32) {
+      if (((uintptr_t)X & 15) == 0 && s.K % per == 0 && s.ld % per == 0 && s.units > NV_CTAS * Q_WARPS && row_bytes * 4u <= NS_SMEM && s.R * s.K >= NS_FROM) {
+        auto stream_rows = [&](auto kern, int rb, int bit) {
+          if (!(d->mx4_quant_attr & (1u << bit))) {
+            if (cudaFuncSetAttribute((const void*)kern, cudaFuncAttributeMaxDynamicSharedMemorySize, NS_SMEM) != cudaSuccess) return launch_status(cudaErrorUnknown);
+            d->mx4_quant_attr |= 1u << bit;
+          }
+          int buffers = NS_SMEM / (int)(row_bytes * (uint32_t)rb);
+          if (buffers > NS_MAX_BUFFERS) buffers = NS_MAX_BUFFERS;
+          const int64_t blocks = (s.R + rb - 1) / rb;
+          return launch_as(0, (size_t)buffers * rb * row_bytes, kern, dim3((unsigned)(blocks < d->sm_count ? blocks : d->sm_count)), 32 * NS_WARPS, stream, x, s, buffers, row_bytes,
+                           buf, flags);
+        };
+        if (row_bytes * 8u <= NS_SMEM) return stream_rows(nv4_quantize_stream_kernel<DT, 4>, 4, 2 * DT);
+        return stream_rows(nv4_quantize_stream_kernel<DT, 2>, 2, 2 * DT + 1);
+      }
     }
     // one unit a warp where the CTAs of a cluster have as many warps, else two; short rows take fewer warps
     const int nu = s.units <= NV_CTAS * Q_WARPS ? 1 : 2;

@@ -272,3 +272,20 @@ def test_weights_quantized_right_in_front_of_the_product(m):
     for _ in range(10):
         for i in (0, 1):
             assert torch.equal(m.sdq_mx4_linear(xq, m.sdq_mx4_quantize(ws[i], buf=buf)), want[i])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("R,K,pad", [(515, 8200, 0), (400, 12000, 8), (261, 16400, 0), (200, 24576, 16)])
+def test_many_long_rows_are_quantized_like_few(m, dtype, R, K, pad):
+    """rows streamed through shared memory (four and two at a time, ragged ends) against the same rows in calls of their own"""
+    x = inputs(R, K + pad, DT[dtype], R).cuda()[:, :K]
+    x[3, 17], x[R - 1, K - 1], x[7, 100] = float("nan"), float("inf"), -float("inf")
+    a = m.mx4_export(m.sdq_mx4_quantize(x, m.FMT_NVFP4))
+    for lo, hi in ((0, 9), (R - 11, R)):
+        b = m.mx4_export(m.sdq_mx4_quantize(x[lo:hi], m.FMT_NVFP4))
+        nan = torch.repeat_interleave(b["scale"] == 127, 8, 1)[:, :b["code"].shape[1]]
+        assert torch.equal(a["scale"][lo:hi], b["scale"]) and torch.equal(a["factor"][lo:hi], b["factor"])
+        assert torch.equal(torch.where(nan, 0, a["code"][lo:hi]), torch.where(nan, 0, b["code"]))
+    check = x[:40].cpu()
+    check_quantized(m, m.sdq_mx4_quantize(x[:40], m.FMT_NVFP4), check, True, False)
+    assert m.device_status() == 0
