@@ -138,8 +138,8 @@ __device__ __forceinline__ Plan make_units(const MoeParams& p, MoeUnit* s_unit, 
 }
 
 // ---- X in pieces ------------------------------------------------------------------------------------------------------------------
-constexpr int SPLIT_THREADS = 256;
-template <int DT>
+// (SPLIT_THREADS: few tokens are spread over more SMs)
+template <int DT, int SPLIT_THREADS>
 __global__ void __launch_bounds__(SPLIT_THREADS)
 moe_split_kernel(const __grid_constant__ MoeParams p)
 {
@@ -233,6 +233,35 @@ struct MoeBars {
   uint32_t tmem, timed_out;
   Plan plan;
 };
+// A producer (one warp): the first lap of the ring at once, a lane a slot, since nothing has to be waited for; then one lane goes on, filling
+// a slot when it has been released.  `fill(i, slot's address, barrier)` starts the copies of step i.
+template <typename F>
+__device__ __forceinline__ void produce(MoeBars& b, const uint8_t* sm, uint32_t slot_bytes, uint32_t slots, uint32_t lane, uint32_t n, uint32_t* flags, F fill) {
+  if (lane < slots && lane < n) fill(lane, ptx::smem_u32(sm) + lane * slot_bytes, ptx::smem_u32(&b.full[lane]));
+  __syncwarp();
+  if (lane == 0) {
+    Slot at(b.full, b.empty, sm, 0);
+    bool ok = true;
+    for (uint32_t i = slots; i < n; ++i) {
+      if (!(ok = wait32(at.empty, at.ph))) break;
+      fill(i, at.at, at.full);
+      at.next(slots, slot_bytes);
+    }
+    if (!ok) atomicOr(&flags[FLAG_TIMEOUT], 1u);
+  }
+  __syncwarp();
+}
+// step counted through a CTA's tasks of `steps` each -> task, step of the task, without a division where it is the one behind the last asked for
+struct Walk {
+  uint32_t steps, i, t, k;
+  __device__ __forceinline__ explicit Walk(uint32_t s) : steps(s), i(0), t(0), k(0) {}
+  __device__ __forceinline__ void to(uint32_t j) {
+    if (j == i + 1) { ++k; if (k == steps) { k = 0; ++t; } }
+    else { t = j / steps; k = j - t * steps; }
+    i = j;
+  }
+};
+
 // the two MMAs (64 K each) of one step; nothing accumulates in front of the first where `acc` is 0
 __device__ __forceinline__ void step_mma(uint32_t d, uint64_t da, uint64_t db, uint32_t sfa, uint32_t sfb, uint32_t id0, uint32_t id2, uint32_t acc) {
   ptx::mma_mxf4(d, da, db, id0, sfa, sfb, acc);
@@ -293,61 +322,54 @@ moe_up_kernel(const __grid_constant__ MoeParams p)
   ptx::cluster_sync();
   ptx::tc_fence_after();
   const int tasks = plan.units * p.tiles_i;
+  const uint32_t n_steps = cluster < tasks ? (uint32_t)((tasks - cluster + clusters - 1) / clusters * steps) : 0u;   // of this CTA
   const uint32_t COLS = (uint32_t)(PIECES * plan.most + 15) / 16 * 16;    // columns of the largest unit there is
   const uint32_t SLOT = SL_B + COLS * 64u + ATOM, NSLOT = min((uint32_t)p.ring_bytes / SLOT, (uint32_t)MOE_MAX_SLOTS), SL_SFB = SL_B + COLS * 64u;
   const uint32_t tmem = b.tmem, bufs = 4 * COLS + 32 <= (uint32_t)p.tmem_cols ? 2u : 1u, sets = tmem + 2 * bufs * COLS;
   bool ok = true;
   if (warp == 0) {
-    if (lane == 0) {
-      Slot at(b.full, b.empty, sm, 1);
-      uint32_t left = NSLOT;                      // slots that have not been used yet
-      for (int task = cluster; task < tasks && ok; task += clusters) {
-        const int u = task / p.tiles_i, tile = task - u * p.tiles_i;
-        const size_t rec = (((size_t)s_unit[u].expert * p.tiles_i + tile) * p.off.sh + k0) * ERECORD;
-        const uint8_t *w1 = p.w1 + rec, *w3 = p.w3 + rec;
-        for (int k = 0; k < steps; ++k, w1 += ERECORD, w3 += ERECORD) {
-          if (left) --left;
-          else if (!(ok = wait32(at.empty, at.ph))) break;
-          expect32(at.full, 2 * ERECORD);
-          copy32(at.at, w1, ERECORD, at.full);
-          copy32(at.at + ERECORD, w3, ERECORD, at.full);
-          at.next(NSLOT, SLOT);
-        }
+    Walk w((uint32_t)steps);
+    auto record = [&](uint32_t i) {               // offset of the step's records
+      w.to(i);
+      const int task = cluster + (int)w.t * clusters, u = task / p.tiles_i, tile = task - u * p.tiles_i;
+      return (((size_t)s_unit[u].expert * p.tiles_i + tile) * p.off.sh + k0 + w.k) * ERECORD;
+    };
+    produce(b, sm, SLOT, NSLOT, lane, n_steps, p.flags, [&](uint32_t i, uint32_t dst, uint32_t bar) {
+      const size_t rec = record(i);
+      expect32(bar, 2 * ERECORD);
+      copy32(dst, p.w1 + rec, ERECORD, bar);
+      copy32(dst + ERECORD, p.w3 + rec, ERECORD, bar);
+      // (while the first lap waits for its activations, the second's weights come into L2)
+      if (i < NSLOT && i + NSLOT < n_steps) {
+        const size_t next = record(i + NSLOT);
+        ptx::bulk_prefetch_l2(p.w1 + next, ERECORD);
+        ptx::bulk_prefetch_l2(p.w3 + next, ERECORD);
+        w.i = i;                                  // (not where the walk goes on)
+        w.t = i / (uint32_t)steps;
+        w.k = i - w.t * (uint32_t)steps;
       }
-      if (!ok) atomicOr(&p.flags[FLAG_TIMEOUT], 1u);
-    }
-    __syncwarp();
+    });
   } else if (warp == 3) {
     // the next launch is let in behind the wait: what lies in front of this one is complete for it
     ptx::griddep_wait();
     if (lane == 0) ptx::griddep_launch_dependents();
   } else if (warp == 2) {
     ptx::griddep_wait();                          // X in pieces
-    if (lane == 0) {
-      Slot at(b.full, b.empty, sm, 1);
-      uint32_t left = NSLOT;
-      for (int task = cluster; task < tasks && ok; task += clusters) {
-        const int u = task / p.tiles_i;
-        const MoeUnit un = s_unit[u];
-        const uint32_t bytes = (uint32_t)(PIECES * un.n + 7) / 8 * GROUP;
-        const size_t stride = (size_t)p.off.groups * GROUP;
-        const uint8_t *x = p.ws + p.off.xp + (size_t)k0 * stride + (size_t)un.group * GROUP, *sf = p.ws + p.off.xs + ((size_t)u * p.off.sh + k0) * ATOM;
-        for (int k = 0; k < steps; ++k, x += stride, sf += ATOM) {
-          if (left) --left;
-          else if (!(ok = wait32(at.empty, at.ph))) break;
-          expect32(at.full, bytes + ATOM);
-          copy32(at.at + SL_B, x, bytes, at.full);
-          copy32(at.at + SL_SFB, sf, ATOM, at.full);
-          at.next(NSLOT, SLOT);
-        }
-      }
-      if (!ok) atomicOr(&p.flags[FLAG_TIMEOUT], 1u);
-    }
-    __syncwarp();
+    Walk w((uint32_t)steps);
+    produce(b, sm, SLOT, NSLOT, lane, n_steps, p.flags, [&](uint32_t i, uint32_t dst, uint32_t bar) {
+      w.to(i);
+      const uint32_t k = w.k;
+      const int u = (cluster + (int)w.t * clusters) / p.tiles_i;
+      const MoeUnit un = s_unit[u];
+      const uint32_t bytes = (uint32_t)(PIECES * un.n + 7) / 8 * GROUP;
+      expect32(bar, bytes + ATOM);
+      copy32(dst + SL_B, p.ws + p.off.xp + ((size_t)(k0 + k) * p.off.groups + un.group) * GROUP, bytes, bar);
+      copy32(dst + SL_SFB, p.ws + p.off.xs + ((size_t)u * p.off.sh + k0 + k) * ATOM, ATOM, bar);
+    });
   } else if (warp == 1) {
     if (lane == 0) {
       Slot at(b.full, b.empty, sm, 0);
-      uint32_t t = 0, sf = sets;
+      uint32_t t = 0, sf = sets, again = n_steps > NSLOT ? n_steps - NSLOT : 0u;      // slots that will be filled again
       const uint64_t a0 = ptx::smem_desc(at.at, 128, 512), b0 = a0 + (SL_B >> 4), c0 = ptx::smem_desc(at.at, 0, 128), cb0 = c0 + (SL_SFB >> 4);
       uint64_t off = 0;
       for (int task = cluster; task < tasks && ok; task += clusters, ++t) {
@@ -363,7 +385,7 @@ moe_up_kernel(const __grid_constant__ MoeParams p)
           ptx::tc_cp_32x128b_warpx4(sf + 8, cb0 + off);
           step_mma(acc, a0 + off, b0 + off, sf, sf + 8, id0, id2, k ? 1u : 0u);
           step_mma(acc + COLS, a0 + off + (ERECORD >> 4), b0 + off, sf + 4, sf + 8, id0, id2, k ? 1u : 0u);
-          commit32(at.empty);
+          if (again) { --again; commit32(at.empty); }
           sf = sets + (sets + 12u - sf);          // (the other set)
           off += SLOT >> 4;
           at.next(NSLOT, SLOT);
@@ -506,54 +528,32 @@ moe_down_kernel(const __grid_constant__ MoeParams p)
   const int g0 = (int)((int64_t)rank * total / ks), g1 = (int)((int64_t)(rank + 1) * total / ks);
   bool ok = true;
   if (warp == 0) {
-    if (lane == 0) {
-      Slot at(b.full, b.empty, sm, 1);
-      uint32_t left = NSLOT;
-      for (int g = g0; g < g1 && ok;) {
-        const int u = g / SI, end = min(g1, (u + 1) * SI);
-        const uint8_t* w2 = p.w2 + (((size_t)s_unit[u].expert * p.tiles_h + tile) * SI + (g - u * SI)) * ERECORD;
-        for (; g < end; ++g, w2 += ERECORD) {
-          if (left) --left;
-          else if (!(ok = wait32(at.empty, at.ph))) break;
-          expect32(at.full, ERECORD);
-          copy32(at.at, w2, ERECORD, at.full);
-          at.next(NSLOT, SLOT);
-        }
-      }
-      if (!ok) atomicOr(&p.flags[FLAG_TIMEOUT], 1u);
-    }
-    __syncwarp();
+    Walk w((uint32_t)SI);
+    produce(b, sm, SLOT, NSLOT, lane, (uint32_t)(g1 - g0), p.flags, [&](uint32_t i, uint32_t dst, uint32_t bar) {
+      w.to((uint32_t)g0 + i);
+      expect32(bar, ERECORD);
+      copy32(dst, p.w2 + (((size_t)s_unit[w.t].expert * p.tiles_h + tile) * SI + w.k) * ERECORD, ERECORD, bar);
+    });
   } else if (warp == 3) {
     // the next launch is let in behind the wait: what lies in front of this one is complete for it
     ptx::griddep_wait();
     if (lane == 0) ptx::griddep_launch_dependents();
   } else if (warp == 2) {
     ptx::griddep_wait();                          // h
-    if (lane == 0) {
-      Slot at(b.full, b.empty, sm, 1);
-      uint32_t left = NSLOT;
-      for (int g = g0; g < g1 && ok;) {
-        const int u = g / SI, end = min(g1, (u + 1) * SI), k = g - u * SI;
-        const MoeUnit un = s_unit[u];
-        const uint32_t bytes = (uint32_t)(PIECES * un.n + 7) / 8 * GROUP;
-        const size_t stride = (size_t)p.off.groups * GROUP;
-        const uint8_t *h = p.ws + p.off.hp + (size_t)k * stride + (size_t)un.group * GROUP, *sf = p.ws + p.off.hs + ((size_t)u * SI + k) * ATOM;
-        for (; g < end; ++g, h += stride, sf += ATOM) {
-          if (left) --left;
-          else if (!(ok = wait32(at.empty, at.ph))) break;
-          expect32(at.full, bytes + ATOM);
-          copy32(at.at + SL_B, h, bytes, at.full);
-          copy32(at.at + SL_SFB, sf, ATOM, at.full);
-          at.next(NSLOT, SLOT);
-        }
-      }
-      if (!ok) atomicOr(&p.flags[FLAG_TIMEOUT], 1u);
-    }
-    __syncwarp();
+    Walk w((uint32_t)SI);
+    produce(b, sm, SLOT, NSLOT, lane, (uint32_t)(g1 - g0), p.flags, [&](uint32_t i, uint32_t dst, uint32_t bar) {
+      w.to((uint32_t)g0 + i);
+      const uint32_t u = w.t, k = w.k;
+      const MoeUnit un = s_unit[u];
+      const uint32_t bytes = (uint32_t)(PIECES * un.n + 7) / 8 * GROUP;
+      expect32(bar, bytes + ATOM);
+      copy32(dst + SL_B, p.ws + p.off.hp + ((size_t)k * p.off.groups + un.group) * GROUP, bytes, bar);
+      copy32(dst + SL_SFB, p.ws + p.off.hs + ((size_t)u * SI + k) * ATOM, ATOM, bar);
+    });
   } else if (warp == 1) {
     if (lane == 0) {
       Slot at(b.full, b.empty, sm, 0);
-      uint32_t seg = 0, sf = sets;
+      uint32_t seg = 0, sf = sets, again = (uint32_t)(g1 - g0) > NSLOT ? (uint32_t)(g1 - g0) - NSLOT : 0u;
       const uint64_t a0 = ptx::smem_desc(at.at, 128, 512), b0 = a0 + (SL_B >> 4), ca0 = ptx::smem_desc(at.at + ECODES, 0, 128), cb0 = ptx::smem_desc(at.at + SL_SFB, 0, 128);
       uint64_t off = 0;
       for (int g = g0; g < g1 && ok; ++seg) {
@@ -567,7 +567,7 @@ moe_down_kernel(const __grid_constant__ MoeParams p)
           ptx::tc_cp_32x128b_warpx4(sf, ca0 + off);
           ptx::tc_cp_32x128b_warpx4(sf + 4, cb0 + off);
           step_mma(acc, a0 + off, b0 + off, sf, sf + 4, id0, id2, more);
-          commit32(at.empty);
+          if (again) { --again; commit32(at.empty); }
           sf = sets + (sets + 8u - sf);
           off += SLOT >> 4;
           at.next(NSLOT, SLOT);
@@ -679,8 +679,9 @@ static sdq_status_t moe(MoeParams p, DeviceInfo* d, void* stream) {
   const uint32_t room = (half ? SMEM_MAX / 2 - 1024 : SMEM_MAX) - 1024 - 128;
   {
     const size_t smem = (size_t)(pairs + 3) / 4 * 4 * 8 + (size_t)p.E * 16;
-    Launch l((unsigned)((p.T * 16 * (int64_t)p.off.sh + SPLIT_THREADS - 1) / SPLIT_THREADS), SPLIT_THREADS, 0, smem, stream);
-    const sdq_status_t st = launch_status(cudaLaunchKernelEx(&l.lc, moe_split_kernel<DT>, p));
+    const int threads = half ? 64 : 256;
+    Launch l((unsigned)((p.T * 16 * (int64_t)p.off.sh + threads - 1) / threads), (unsigned)threads, 0, smem, stream);
+    const sdq_status_t st = launch_status(half ? cudaLaunchKernelEx(&l.lc, moe_split_kernel<DT, 64>, p) : cudaLaunchKernelEx(&l.lc, moe_split_kernel<DT, 256>, p));
     if (st != SDQ_OK) return st;
   }
   {

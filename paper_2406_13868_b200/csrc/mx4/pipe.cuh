@@ -7,9 +7,13 @@
 namespace sdq {
 namespace mx4 {
 
-__device__ __forceinline__ bool wait32(uint32_t bar, uint32_t parity) {
+__device__ __forceinline__ bool test32(uint32_t bar, uint32_t parity) {
   uint32_t ok;
   asm volatile("{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ bool wait32(uint32_t bar, uint32_t parity) {
+  uint32_t ok = test32(bar, parity);
   for (uint32_t i = 0; !ok && i < (1u << 22); ++i)
     asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok != 0;
