@@ -44,7 +44,7 @@ def _build_binding() -> None:
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden",
            "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI)] + ["-I" + i for i in inc]
     # torch's own libraries are in the process already (the package imports torch first); libsdq_b200.so sits beside this file
-    cmd += ["-o", BINDING + ".tmp", BINDING_SOURCE, "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda",
+    cmd += ["-o", BINDING + ".tmp", BINDING_SOURCE, "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda",
             "-L" + _HERE, "-l:libsdq_b200.so", "-Wl,-rpath,$ORIGIN"]
     subprocess.check_call(cmd, cwd=CSRC)
     os.replace(BINDING + ".tmp", BINDING)

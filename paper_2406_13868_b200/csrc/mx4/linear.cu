@@ -56,20 +56,6 @@ constexpr int NARROW_MAX_SLOTS = 12;
 // slot = | weight record | codes of T tokens | scale atoms of the tokens |
 __host__ __device__ constexpr uint32_t narrow_slot(int fmt, int T) { return record(fmt) + (uint32_t)T * 128u + atoms(fmt) * ATOM; }
 
-// sum over the cluster's CTAs, in their order, of the four floats at `local`; all of them are asked for before the first is added
-__device__ __forceinline__ float4 sum_over_cluster(const float* local, uint32_t ctas) {
-  const uint32_t at = ptx::smem_u32(local);
-  float4 v[8];
-#pragma unroll
-  for (uint32_t c = 0; c < 8; ++c)
-    if (c < ctas) v[c] = ptx::ld_cluster_f32x4(ptx::mapa_u32(at, c));
-  float4 s = v[0];
-#pragma unroll
-  for (uint32_t c = 1; c < 8; ++c)
-    if (c < ctas) { s.x += v[c].x; s.y += v[c].y; s.z += v[c].z; s.w += v[c].w; }
-  return s;
-}
-
 template <int FMT, int DT>
 __global__ void __launch_bounds__(NARROW_THREADS)
 mx4_linear_narrow_kernel(const __grid_constant__ GemmParams p)

@@ -487,7 +487,7 @@ moe_up_kernel(const __grid_constant__ MoeParams p)
 // ---- W2 h, and the sum over a token's pairs -------------------------------------------------------------------------------------
 // A cluster has one tile of 128 outputs; its CTAs share the steps of all units.  slot = | record of W2 | columns of h | scale atom |
 template <int DT>
-__global__ void __launch_bounds__(MOE_THREADS)
+__global__ void __launch_bounds__(MOE_THREADS, 2)
 moe_down_kernel(const __grid_constant__ MoeParams p)
 {
   using T = typename std::conditional<DT == SDQ_BF16, __nv_bfloat16, __half>::type;
@@ -618,14 +618,10 @@ moe_down_kernel(const __grid_constant__ MoeParams p)
   __syncthreads();
   ptx::cluster_sync();
   ptx::griddep_wait();                             // (all threads: Y may be in use by a kernel in front)
-  for (uint32_t i = tid; i < 32u * (uint32_t)p.T; i += MOE_THREADS) {
-    if (i % ks != rank) continue;
+  // (neighbouring threads of a CTA on neighbouring outputs; dealt out one by one among the CTAs, the loads cost 10 us at 64 tokens)
+  for (uint32_t i = rank * MOE_THREADS + tid; i < 32u * (uint32_t)p.T; i += ks * MOE_THREADS) {
     const int t = (int)(i >> 5), r0 = (int)(i & 31u) * 4;
-    float4 s = make_float4(0, 0, 0, 0);
-    for (uint32_t c = 0; c < ks; ++c) {
-      const float4 v = load_cta4(out + t * 128 + r0, c);
-      s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
-    }
+    const float4 s = sum_over_cluster(out + t * 128 + r0, ks);
     const int64_t n = (int64_t)tile * 128 + r0;
     T* y = reinterpret_cast<T*>(p.y) + (int64_t)t * p.ldy + n;
     const float v[4] = {s.x, s.y, s.z, s.w};

@@ -30,6 +30,19 @@ __device__ __forceinline__ void commit32(uint32_t bar) {
 // the two halves of ptx::cluster_sync
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// sum over the cluster's CTAs (up to eight), in their order, of the four floats at `local`; all of them are asked for before the first is added
+__device__ __forceinline__ float4 sum_over_cluster(const float* local, uint32_t ctas) {
+  const uint32_t at = ptx::smem_u32(local);
+  float4 v[8];
+#pragma unroll
+  for (uint32_t c = 0; c < 8; ++c)
+    if (c < ctas) v[c] = ptx::ld_cluster_f32x4(ptx::mapa_u32(at, c));
+  float4 s = v[0];
+#pragma unroll
+  for (uint32_t c = 1; c < 8; ++c)
+    if (c < ctas) { s.x += v[c].x; s.y += v[c].y; s.z += v[c].z; s.w += v[c].w; }
+  return s;
+}
 // position in a ring of `n` slots: barriers 8 bytes apart, data `size` bytes apart; `ph` flips with every lap
 struct Slot {
   uint32_t s, ph, full, empty, at;

@@ -11,6 +11,7 @@
 #include <vector>
 
 #include <ATen/core/Tensor.h>
+#include <ATen/cuda/EmptyTensor.h>
 #include <ATen/ops/empty.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -420,7 +421,8 @@ bool to_int(PyObject* o, int64_t& v) {
   if (v == -1 && PyErr_Occurred()) { PyErr_Clear(); return false; }
   return v >= INT32_MIN && v <= INT32_MAX;
 }
-at::TensorOptions on(const at::Tensor& t, at::ScalarType type) { return at::TensorOptions().dtype(type).device(t.device()); }
+// a new tensor beside `t`, without the dispatcher's way to the same function
+at::Tensor fresh(const at::Tensor& t, at::IntArrayRef size, at::ScalarType type) { return at::detail::empty_cuda(size, type, t.device(), std::nullopt); }
 
 // mx4_quantize(X, fmt, rule, buf or None) -> Mx4Matrix
 PyObject* mx4_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
@@ -435,7 +437,7 @@ PyObject* mx4_quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
     size_t bytes = 0;
     const sdq_status_t st = sdq_mx4_size(R, K, (int32_t)fmt, &bytes);
     if (st != SDQ_OK) return raise(st, "sdq_mx4_size");
-    buf = at::empty({(int64_t)bytes}, on(*X, at::kByte));
+    buf = fresh(*X, {(int64_t)bytes}, at::kByte);
   } else {
     const at::Tensor* b = dense(a[3], at::kByte, 1);
     if (!b) NOT_HERE;
@@ -480,7 +482,7 @@ PyObject* mx4_linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
   }
   at::Tensor out;
   if (a[3] == Py_None) {
-    out = at::empty({x.q->R, w.q->R}, on(THPVariable_Unpack(w.buf.get()), type));
+    out = fresh(THPVariable_Unpack(w.buf.get()), {x.q->R, w.q->R}, type);
   } else {
     const at::Tensor* o = matrix(a[3], (int)dt);
     if (!o || o->size(0) != x.q->R || o->size(1) != w.q->R) NOT_HERE;
@@ -504,8 +506,9 @@ PyObject* mx4_dequantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (n != 2 || !to_int(a[1], dt) || dt < SDQ_BF16 || dt > SDQ_FP32) NOT_HERE;
   Mx4 q(a[0]);
   if (!q.q) NOT_HERE;
-  const at::TensorOptions opt = on(THPVariable_Unpack(q.buf.get()), dt == SDQ_BF16 ? at::kBFloat16 : dt == SDQ_FP16 ? at::kHalf : at::kFloat);
-  at::Tensor out = q.q->E ? at::empty({q.q->E, q.q->R, q.q->K}, opt) : at::empty({q.q->R, q.q->K}, opt);
+  const at::Tensor& b = THPVariable_Unpack(q.buf.get());
+  const at::ScalarType type = dt == SDQ_BF16 ? at::kBFloat16 : dt == SDQ_FP16 ? at::kHalf : at::kFloat;
+  at::Tensor out = q.q->E ? fresh(b, {q.q->E, q.q->R, q.q->K}, type) : fresh(b, {q.q->R, q.q->K}, type);
   void *y = out.data_ptr(), *stream = current_stream();
   sdq_status_t st;
   Py_BEGIN_ALLOW_THREADS
@@ -535,7 +538,7 @@ PyObject* moe_route(PyObject*, PyObject* const* a, Py_ssize_t n) {
     bias = (const float*)b->data_ptr();
   }
   const int64_t T = X->size(0), H = X->size(1), E = W->size(0);
-  at::Tensor ids = at::empty({T, k}, on(*X, at::kInt)), weights = at::empty({T, k}, on(*X, at::kFloat));
+  at::Tensor ids = fresh(*X, {T, k}, at::kInt), weights = fresh(*X, {T, k}, at::kFloat);
   void *x = X->data_ptr(), *w = W->data_ptr(), *i = ids.data_ptr(), *v = weights.data_ptr(), *stream = current_stream();
   const int64_t ldx = row_stride(*X), ldw = row_stride(*W);
   const float scale = (float)PyFloat_AS_DOUBLE(a[6]);
@@ -562,7 +565,7 @@ PyObject* mx4_moe(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const int dt = mx4_dtype(X->scalar_type());
   at::Tensor out, ws;
   if (a[6] == Py_None) {
-    out = at::empty({T, H}, on(*X, X->scalar_type()));
+    out = fresh(*X, {T, H}, X->scalar_type());
   } else {
     const at::Tensor* o = matrix(a[6], dt);
     if (!o || o->size(0) != T || o->size(1) != H) NOT_HERE;
@@ -572,7 +575,7 @@ PyObject* mx4_moe(PyObject*, PyObject* const* a, Py_ssize_t n) {
     size_t bytes = 0;
     const sdq_status_t st = sdq_mx4_moe_workspace_size(T, (int32_t)k, H, w1.q->R, &bytes);
     if (st != SDQ_OK) return raise(st, "sdq_mx4_moe_workspace_size");
-    ws = at::empty({(int64_t)bytes}, on(*X, at::kByte));
+    ws = fresh(*X, {(int64_t)bytes}, at::kByte);
   } else {
     const at::Tensor* w = dense(a[7], at::kByte, 1);
     if (!w) NOT_HERE;
