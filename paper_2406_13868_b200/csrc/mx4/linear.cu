@@ -482,6 +482,26 @@ static cudaError_t with_smem(K kern, uint32_t bytes, DeviceInfo* d, int bit) {
 }
 constexpr uint32_t SMEM_MAX = 232448;
 
+// CTAs that share K of a row tile in the narrow kernel: as many as keep all of them resident, two an SM, with a tenth left over for clusters
+// that do not fit a GPU processing cluster (96 tiles x 3 of K = 4096 took 16.2 us, x 2 11.1); the sum over them is the dearer the more tokens there are
+// (128 tokens, 4096 x 4096: four 7.7 us, eight 10.4; 16 tokens, 11008 -> 4096: four 9.8, eight 8.8; 64 tokens, 8192 -> 512: four 6.7, eight 5.4).
+static int narrow_split(int64_t tiles, int T, int kb, int sms) {
+  int ks = 1;
+  for (int k = 2; k <= (T > 32 && 8 * tiles > sms ? 4 : 8) && k <= kb; ++k)
+    if (10 * k * tiles <= 18 * sms) ks = k;
+  return ks;
+}
+// Which kernel takes a call of more than 128 tokens: microseconds that each took, as linear functions of what its longest CTA goes through (sweeps
+// of 129 to 1500 tokens against 1000 to 11008 rows, K 1000 to 11008, within 15 %).  E.g. MXFP4, narrow and wide: 256 x 4096 -> 4096 10.1 and 11.4, 333 x 4096 -> 11008
+// 13.7 and 20.4, 512 x 11008 -> 4096 18.2 and 22.0, 256 x 4096 -> 11008 13.6 and 12.9, 512 x 4096 -> 11008 24.0 and 20.4
+static bool narrow_is_faster(int fmt, int64_t tiles, int ks, int64_t wide_tasks, int kb, bool aligned, int sms) {
+  const bool nv = fmt == SDQ_FMT_NVFP4;
+  const int64_t waves = (tiles * ks + 2 * sms - 1) / (2 * sms), wide_waves = (wide_tasks + sms / 2 - 1) / (sms / 2);
+  const double narrow = (double)waves * ((kb <= 8 ? 5.0 : 8.2) + (nv ? 0.55 : 0.44) * (double)((kb + ks - 1) / ks));
+  const double wide = (aligned ? 3.4 : 4.9) + (double)wide_waves * (2.2 + (nv ? 0.433 : 0.374) * kb);
+  return narrow < wide;
+}
+
 template <int FMT, int DT>
 static sdq_status_t linear(GemmParams& p, DeviceInfo* d, void* stream) {
   cudaLaunchConfig_t lc = {};
@@ -495,16 +515,14 @@ static sdq_status_t linear(GemmParams& p, DeviceInfo* d, void* stream) {
   lc.numAttrs = 2;
   lc.stream = (cudaStream_t)stream;
   constexpr int BIT = 3 * (FMT * 3 + DT);
-  if (p.M <= 512) {
-    p.T = p.M <= 128 ? (int32_t)(p.M + 15) / 16 * 16 : 128;
-    const int64_t tiles = (int64_t)p.n_tiles * p.m_tiles;
-    // K over as many CTAs as leave the fullest SM the fewest records, two CTAs an SM at most; of equal ones the fewest
-    int ks = 1;
-    int64_t least = 0;
-    for (int k = 1; k <= 8 && k <= p.kb && (k == 1 || k * tiles <= 2 * d->sm_count); ++k) {
-      const int64_t most = ((k * tiles + d->sm_count - 1) / d->sm_count) * ((p.kb + k - 1) / k);
-      if (k == 1 || most < least) { ks = k; least = most; }
-    }
+  p.T = p.M <= 128 ? (int32_t)(p.M + 15) / 16 * 16 : 128;
+  const int64_t tiles = (int64_t)p.n_tiles * p.m_tiles;
+  const int ks = narrow_split(tiles, p.T, p.kb, d->sm_count);
+  p.pt_m = (p.m_tiles + 1) / 2;
+  p.pt_n = (p.n_tiles + 1) / 2;
+  const int64_t sector = 32 / (int64_t)dtype_bytes(DT);
+  const bool vec = ((uintptr_t)p.Y & 31) == 0 && p.ldy % sector == 0 && p.N % sector == 0;      // rows of Y in whole 32-byte sectors
+  if (p.M <= 128 || narrow_is_faster(FMT, tiles, ks, (int64_t)p.pt_m * p.pt_n, p.kb, vec, d->sm_count)) {
     const uint32_t slot = narrow_slot(FMT, p.T);
     const uint32_t room = (tiles * ks <= d->sm_count ? SMEM_MAX : SMEM_MAX / 2 - 1024) - NARROW_TAIL;
     const int want = (p.kb + ks - 1) / ks;
@@ -526,16 +544,12 @@ static sdq_status_t linear(GemmParams& p, DeviceInfo* d, void* stream) {
     if (with_smem(kern, SMEM_MAX, d, BIT) != cudaSuccess) return launch_status(cudaErrorUnknown);
     return launch_status(cudaLaunchKernelEx(&lc, kern, p));
   }
-  p.pt_m = (p.m_tiles + 1) / 2;
-  p.pt_n = (p.n_tiles + 1) / 2;
   if ((int64_t)p.pt_m * p.pt_n > 0x3FFFFFFF) return SDQ_ERR_SHAPE;
   p.tasks = p.pt_m * p.pt_n;
   const int pairs = d->sm_count / 2 < p.tasks ? d->sm_count / 2 : p.tasks;
   lc.gridDim = dim3(2 * (unsigned)pairs);
   lc.blockDim = dim3(WIDE_THREADS);
   attr[1].val.clusterDim.x = 2;
-  const int64_t sector = 32 / (int64_t)dtype_bytes(DT);
-  const bool vec = ((uintptr_t)p.Y & 31) == 0 && p.ldy % sector == 0 && p.N % sector == 0;
   auto go = [&](auto kern, auto v, int bit) {
     constexpr bool V = decltype(v)::value;
     constexpr uint32_t bytes = wide_slots(FMT, V) * wide_slot(FMT) + wide_tail(V);
