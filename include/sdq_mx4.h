@@ -49,7 +49,7 @@ sdq_status_t sdq_mx4_quantize(const void* X, int32_t dtype, int64_t R, int64_t K
                               void* buf, size_t bytes, sdq_mx4_t* out, void* stream);
 
 /* Codes and scales as checkpoints hold them -> the tiled layout.  codes (device) [R][ceil(K/2)], two to a byte, the lower k in the
- * low nibble; scales (device) [R][ceil(K/32)] E8M0 or [R][ceil(K/16)] E4M3; factor (device) [R] fp32, NVFP4 only, NULL = 1. */
+ * low nibble; scales (device) [R][ceil(K/32)] E8M0 or [R][ceil(K/16)] E4M3 (its sign bit is not looked at); factor (device) [R] fp32, NVFP4 only, NULL = 1. */
 sdq_status_t sdq_mx4_import(const uint8_t* codes, const uint8_t* scales, const float* factor, int64_t R, int64_t K, int32_t fmt,
                             void* buf, size_t bytes, sdq_mx4_t* out, void* stream);
 

@@ -81,7 +81,6 @@ mx4_linear_narrow_kernel(const __grid_constant__ GemmParams p)
 
   if (warp == 0) {
     if (lane == 0) {
-      ptx::griddep_launch_dependents();
       for (uint32_t i = 0; i < NSLOT; ++i) { ptx::mbar_init(&full[i], 2); ptx::mbar_init(&empty[i], 1); }
       ptx::mbar_init(acc_full, 1);
       ptx::fence_barrier_init();
@@ -95,8 +94,9 @@ mx4_linear_narrow_kernel(const __grid_constant__ GemmParams p)
   ptx::tc_fence_before();
   __syncthreads();
   ptx::tc_fence_after();
-  const uint32_t tmem = *tmem_slot, sets = tmem + (T <= 128 ? 128u : T);
+  const uint32_t tmem = *tmem_slot, sets = tmem + 128u;
   ptx::griddep_wait();
+  if (tid == 0) ptx::griddep_launch_dependents();
 
   bool ok = true;
   if (warp == 0 || warp == 2) {
@@ -254,7 +254,6 @@ mx4_linear_wide_kernel(const __grid_constant__ GemmParams p)
   const int KB = p.kb;
 
   if (warp == 0 && lane == 0) {
-    ptx::griddep_launch_dependents();
     for (int i = 0; i < WIDE_SLOTS; ++i) ptx::mbar_init(&full[i], 1);
     for (int i = 0; i < WIDE_SETS; ++i) ptx::mbar_init(&scales[i], 8);
     for (int i = 0; i < WIDE_PAIRS; ++i) ptx::mbar_init(&empty[i], 1);
@@ -271,6 +270,7 @@ mx4_linear_wide_kernel(const __grid_constant__ GemmParams p)
   ptx::tc_fence_after();
   const uint32_t tmem = *tmem_slot, sets = tmem + 256u;
   ptx::griddep_wait();
+  if (tid == 0) ptx::griddep_launch_dependents();
 
   // task -> tiles of 256: weight tiles vary fastest inside bands of eight token tiles
   auto tile_of = [&](int task, int& mt, int& nt) {
@@ -522,14 +522,14 @@ static sdq_status_t linear(GemmParams& p, DeviceInfo* d, void* stream) {
   p.pt_n = (p.n_tiles + 1) / 2;
   const int64_t sector = 32 / (int64_t)dtype_bytes(DT);
   const bool vec = ((uintptr_t)p.Y & 31) == 0 && p.ldy % sector == 0 && p.N % sector == 0;      // rows of Y in whole 32-byte sectors
-  if (p.M <= 128 || narrow_is_faster(FMT, tiles, ks, (int64_t)p.pt_m * p.pt_n, p.kb, vec, d->sm_count)) {
+  if (p.M <= 128 || p.m_tiles <= 65535 && narrow_is_faster(FMT, tiles, ks, (int64_t)p.pt_m * p.pt_n, p.kb, vec, d->sm_count)) {
     const uint32_t slot = narrow_slot(FMT, p.T);
     const uint32_t room = (tiles * ks <= d->sm_count ? SMEM_MAX : SMEM_MAX / 2 - 1024) - NARROW_TAIL;
     const int want = (p.kb + ks - 1) / ks;
     p.nslot = (int32_t)(room / slot);
     if (p.nslot > want) p.nslot = want;
     if (p.nslot > NARROW_MAX_SLOTS) p.nslot = NARROW_MAX_SLOTS;
-    if (p.n_tiles > 0x7FFFFFFF / 8 || p.m_tiles > 65535) return SDQ_ERR_SHAPE;
+    if (p.n_tiles > 0x7FFFFFFF / 8) return SDQ_ERR_SHAPE;
     const uint32_t ring = (uint32_t)p.nslot * slot, parts = (uint32_t)p.T * ROWS * 4u;
     // (the partial tile lies where the ring was; the barriers behind both)
     if (parts > ring) p.nslot = (int32_t)((parts + slot - 1) / slot);

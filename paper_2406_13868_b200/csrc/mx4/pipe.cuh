@@ -1,6 +1,10 @@
 // The ring's operations on 32-bit shared-memory addresses.  One thread fills a ring and one thread empties it, and a trip of either loop has to be
 // shorter than what it moves takes: a thread alone issues an instruction every few clocks, so addresses and descriptors are kept and
 // stepped instead of being worked out in every trip.
+//
+// Every kernel of this directory lets the next launch in behind its own wait for the one in front (griddepcontrol.launch_dependents after
+// griddepcontrol.wait).  A launch may then read, in front of its own wait, what was complete before the launch in front of it began to work:
+// the library's other products read packed weights there, this directory's expert layer ids and experts' weights.
 #pragma once
 #include "../sdq_ptx.cuh"
 

@@ -358,8 +358,8 @@ __global__ void __launch_bounds__(32 * Q_WARPS)
 mx4_quantize_kernel(const typename Elem<DT>::type* __restrict__ X, Shape s, int ceil_rule, uint8_t* __restrict__ buf)
 {
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  if (threadIdx.x == 0) ptx::griddep_launch_dependents();
   ptx::griddep_wait();
+  if (threadIdx.x == 0) ptx::griddep_launch_dependents();       // (behind the wait: see pipe.cuh)
   const int64_t g = blockIdx.x, r = element_row<EXPERTS>(g, s.R, s.tiles, lane);
   const Bounds m = bounds_of<DT>(X, s);
   for (int64_t u = (int64_t)blockIdx.y * (blockDim.x >> 5) + warp; u < s.units; u += (int64_t)gridDim.y * (blockDim.x >> 5)) {
@@ -411,8 +411,8 @@ nv4_quantize_kernel(const typename Elem<DT>::type* __restrict__ X, Shape s, uint
 {
   __shared__ NvMax mx;
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-  if (threadIdx.x == 0) ptx::griddep_launch_dependents();
   ptx::griddep_wait();
+  if (threadIdx.x == 0) ptx::griddep_launch_dependents();       // (behind the wait: see pipe.cuh)
   const uint32_t ctas = LONG ? 1u : gridDim.y, rank = LONG ? 0u : blockIdx.y;
   const int64_t g = blockIdx.x, r = element_row<false>(g, s.R, s.tiles, lane);
   const Bounds m = bounds_of<DT>(X, s);
@@ -497,10 +497,10 @@ nv4_quantize_stream_kernel(const typename Elem<DT>::type* __restrict__ X, Shape 
   if (tid == 0) {
     for (int n = 0; n < buffers; ++n) ptx::mbar_init(&full[n], 1);
     ptx::fence_barrier_init();
-    ptx::griddep_launch_dependents();
   }
   __syncthreads();
   ptx::griddep_wait();
+  if (tid == 0) ptx::griddep_launch_dependents();
   if (tid == 0)
     for (int n = 0; n < buffers; ++n)
       if (blockIdx.x + (int64_t)n * gridDim.x < blocks) load(blockIdx.x + (int64_t)n * gridDim.x, n);
@@ -582,8 +582,8 @@ __global__ void __launch_bounds__(32 * Q_WARPS)
 mx4_import_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, const float* __restrict__ factor, Shape s, uint8_t* __restrict__ buf)
 {
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  if (threadIdx.x == 0) ptx::griddep_launch_dependents();
   ptx::griddep_wait();
+  if (threadIdx.x == 0) ptx::griddep_launch_dependents();       // (behind the wait: see pipe.cuh)
   const int64_t g = blockIdx.x, r = element_row<EXPERTS>(g, s.R, s.tiles, lane);
   const int64_t kb = (s.K + 1) / 2, nb = FMT == SDQ_FMT_NVFP4 ? (s.K + 15) / 16 : (s.K + 31) / 32;
   for (int64_t u = (int64_t)blockIdx.y * Q_WARPS + warp; u < s.units; u += (int64_t)gridDim.y * Q_WARPS) {
@@ -604,7 +604,7 @@ mx4_import_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__
             w[i / 4] |= c << (8 * (i % 4));
           }
         }
-        if (sb < nb) sc[h] = scales[r * nb + sb];
+        if (sb < nb) sc[h] = scales[r * nb + sb] & (FMT == SDQ_FMT_NVFP4 ? 0x7Fu : 0xFFu);
       }
       if (on) put_codes(x, h, make_uint2(w[0], w[1]));
     }
@@ -618,8 +618,8 @@ __global__ void __launch_bounds__(32 * Q_WARPS)
 mx4_export_kernel(uint8_t* __restrict__ buf, Shape s, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales, float* __restrict__ factor)
 {
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  if (threadIdx.x == 0) ptx::griddep_launch_dependents();
   ptx::griddep_wait();
+  if (threadIdx.x == 0) ptx::griddep_launch_dependents();       // (behind the wait: see pipe.cuh)
   const int64_t g = blockIdx.x, r = element_row<EXPERTS>(g, s.R, s.tiles, lane);
   if (r < 0) return;
   const int64_t kb = (s.K + 1) / 2, nb = FMT == SDQ_FMT_NVFP4 ? (s.K + 15) / 16 : (s.K + 31) / 32;
@@ -659,8 +659,8 @@ mx4_dequantize_kernel(uint8_t* __restrict__ buf, Shape s, typename Elem<DT>::typ
   constexpr int W = 16 * sizeof(T) / 4;
   __shared__ __align__(16) uint8_t stage[VEC ? 16 : Q_WARPS * Stage<DT>::BYTES];
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  if (threadIdx.x == 0) ptx::griddep_launch_dependents();
   ptx::griddep_wait();
+  if (threadIdx.x == 0) ptx::griddep_launch_dependents();       // (behind the wait: see pipe.cuh)
   const int64_t g = blockIdx.x, r = element_row<EXPERTS>(g, s.R, s.tiles, lane);
   uint8_t* st = stage + (VEC ? 0 : warp * Stage<DT>::BYTES);
   float f = 1.0f;

@@ -206,8 +206,8 @@ moe_route_mma_kernel(const __grid_constant__ RouteParams p)
   const int chunks = (int)((p.H + 31) / 32), parts = p.splits * ROUTE_WARPS, part = split * ROUTE_WARPS + (int)warp;
   const int c0 = (int)((int64_t)part * chunks / parts), c1 = (int)((int64_t)(part + 1) * chunks / parts);
   cluster_arrive();
-  if (tid == 0) ptx::griddep_launch_dependents();
   ptx::griddep_wait();
+  if (tid == 0) ptx::griddep_launch_dependents();
   const bool token = t0 + r < p.T;
   const uint16_t* x = X + (token ? t0 + r : 0) * p.ldx + c8;
   bool waited = false;
@@ -290,8 +290,8 @@ moe_route_kernel(const __grid_constant__ RouteParams p)
   uint32_t ctas;
   asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(ctas));
   const uint32_t rank = ptx::cluster_ctarank();
-  if (threadIdx.x == 0) ptx::griddep_launch_dependents();
   ptx::griddep_wait();
+  if (threadIdx.x == 0) ptx::griddep_launch_dependents();
   const int64_t t0 = (int64_t)(blockIdx.x / ctas) * G;
   const T* X = reinterpret_cast<const T*>(p.x);
   const T* W = reinterpret_cast<const T*>(p.w);

@@ -31,8 +31,18 @@ def test_no_remote_shared_memory_before_the_cluster_has_started(bodies):
         assert syncs[0] < first and syncs[-1] > last, n
 
 
+def test_every_kernel_lets_the_next_launch_in_behind_its_own_wait(bodies):
+    """a launch may read, in front of its own wait, what was complete before the launch in front of it began: the library's products read packed
+    weights there, the expert layer ids and weights"""
+    assert len(bodies) >= 12
+    for n, b in bodies.items():
+        lets_in = [x.start() for x in re.finditer(r"griddep_launch_dependents\(\)", b)]
+        assert len(lets_in) == 1, n
+        assert re.search(r"ptx::griddep_wait\(\);\s*if \((?:lane|tid|threadIdx\.x) == 0\) $", b[:lets_in[0] - len("ptx::")]), n
+
+
 def test_global_memory_is_read_behind_the_wait_for_the_launch_in_front(bodies):
-    """every kernel that lets the next launch in at once waits before its first copy; only a prefetch into L2 may come earlier"""
+    """only a prefetch into L2 may come earlier: the launch in front may be the one that writes a weight matrix"""
     for n, b in bodies.items():
         if n in ("moe_up_kernel", "moe_down_kernel"):
             continue
@@ -42,13 +52,8 @@ def test_global_memory_is_read_behind_the_wait_for_the_launch_in_front(bodies):
 
 
 def test_expert_layer_reads_ids_and_weights_early_only_behind_launches_that_have_waited(bodies):
-    """the products read ids and expert weights in front of their own wait, so the launches in front of them, the layer's own, let them in
-    behind theirs; the scratch, the tokens and the outputs are touched behind the wait"""
-    for n in ("moe_split_kernel", "moe_up_kernel", "moe_down_kernel"):
-        b = bodies[n]
-        lets_in = [x.start() for x in re.finditer(r"griddep_launch_dependents\(\)", b)]
-        assert len(lets_in) == 1
-        assert re.search(r"ptx::griddep_wait\(\);\s*if \((?:lane|tid) == 0\) $", b[:lets_in[0] - len("ptx::")])
+    """the products read ids and expert weights in front of their own wait, which the launches in front of them, the layer's own, allow;
+    the scratch, the tokens and the outputs are touched behind the wait"""
     for n in ("moe_up_kernel", "moe_down_kernel"):
         b = bodies[n]
         roles = re.split(r"\} else if \(warp", b[b.index("bool ok = true"):])
