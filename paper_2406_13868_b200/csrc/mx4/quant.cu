@@ -24,11 +24,6 @@ template <> struct Elem<SDQ_FP32> { using type = float; };
 template <int DT> __device__ __forceinline__ constexpr float type_max() {
   return DT == SDQ_BF16 ? 3.3895313892515355e38f : DT == SDQ_FP16 ? 65504.0f : 3.4028234663852886e38f;
 }
-template <int DT> __device__ __forceinline__ float to_float(typename Elem<DT>::type x) {
-  if constexpr (DT == SDQ_BF16) return __bfloat162float(x);
-  else if constexpr (DT == SDQ_FP16) return __half2float(x);
-  else return x;
-}
 template <int DT> __device__ __forceinline__ typename Elem<DT>::type from_float(float x) {
   if constexpr (DT == SDQ_BF16) return __float2bfloat16_rn(x);
   else if constexpr (DT == SDQ_FP16) return __float2half_rn(x);

@@ -5,9 +5,6 @@
 // operands are exact in fp32, 32 of them are summed there, by the tensor core (mma.sync: sixteen experts x eight tokens, a shape that
 // this size of problem fills, where a tcgen05 tile would be all padding), and everything behind that in 64 bits.  fp32 operands go through
 // ordinary multiplications, eight to a sum.
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
-
 #include "../sdq_internal.h"
 #include "../sdq_ptx.cuh"
 #include "layout.h"
@@ -19,35 +16,20 @@ namespace mx4 {
 constexpr int ROUTE_WARPS = 16, ROUTE_CTAS = 8;
 constexpr int ROUTE_MAX_E = 1024, ROUTE_MAX_K = 32;
 
-template <int DT> struct RouteElem;
-template <> struct RouteElem<SDQ_BF16> { using type = __nv_bfloat16; };
-template <> struct RouteElem<SDQ_FP16> { using type = __half; };
-template <> struct RouteElem<SDQ_FP32> { using type = float; };
-template <int DT> __device__ __forceinline__ float route_float(typename RouteElem<DT>::type x) {
-  if constexpr (DT == SDQ_BF16) return __bfloat162float(x);
-  else if constexpr (DT == SDQ_FP16) return __half2float(x);
-  else return x;
-}
 // eight consecutive elements; `n` of them exist (VEC: all or none)
-template <int DT, bool VEC>
-__device__ __forceinline__ void load8(float (&v)[8], const typename RouteElem<DT>::type* p, int64_t n) {
-  using T = typename RouteElem<DT>::type;
-  if constexpr (VEC && DT != SDQ_FP32) {
-    uint4 r = make_uint4(0, 0, 0, 0);
-    if (n > 0) r = __ldg(reinterpret_cast<const uint4*>(p));
-    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+template <bool VEC>
+__device__ __forceinline__ void load8(float (&v)[8], const float* p, int64_t n) {
+  if constexpr (VEC) {
+    // (no branch: loads of a batch go out together)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if constexpr (DT == SDQ_BF16) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
-      else { const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i])); v[2 * i] = f.x; v[2 * i + 1] = f.y; }
-    }
-  } else if constexpr (VEC) {
-    float4 a = make_float4(0, 0, 0, 0), b = a;
-    if (n > 0) { a = __ldg(reinterpret_cast<const float4*>(p)); b = __ldg(reinterpret_cast<const float4*>(p) + 1); }
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %5, 0;\n@p ld.global.nc.v4.f32 {%0, %1, %2, %3}, [%4];\n}"
+                   : "+f"(v[4 * i]), "+f"(v[4 * i + 1]), "+f"(v[4 * i + 2]), "+f"(v[4 * i + 3]) : "l"(p + 4 * i), "r"((uint32_t)(n > 0)));
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < n ? route_float<DT>(p[i]) : 0.0f;
+    for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : 0.0f;
   }
 }
 // order of doubles as order of integers: of equal ones the two zeros alike, a NaN above everything
@@ -75,27 +57,27 @@ struct RouteParams {
   float scale;
 };
 
-// one token's scores, choices and weights, by all warps of the CTA.  score: [E] logits; key: [E]; red: scratch of ROUTE_WARPS doubles.
-// A softmax is left undivided where only the order and the ratios of the scores matter.
+// one token's scores, choices and weights, by all warps of the CTA.  score: [E] logits; key: [E]; red: scratch of ROUTE_WARPS doubles and 2 ROUTE_COUNTED
+// words.  A softmax is left undivided where only the order and the ratios of the scores matter.
+// Up to ROUTE_COUNTED experts the choice is by counting (64 experts, 6 of them: 4.8 us a call, against 5.6 with six maxima one behind the other; 256
+// experts, 8 of them: 12.0 against 9.3).
+constexpr int ROUTE_COUNTED = 128;
 __device__ __forceinline__ void choose(const RouteParams& p, int64_t t, double* score, long long* key, double* red) {
   const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   constexpr int THREADS = 32 * ROUTE_WARPS;
+  int32_t *place = reinterpret_cast<int32_t*>(red + ROUTE_WARPS), *chosen = place + ROUTE_COUNTED;
   double inv = 1.0;
   if (!p.sigmoid) {
-    // the exponentials are formed relative to a number near the largest logit: the fp32 one
+    // the exponentials are formed relative to a number near the largest logit: the fp32 one (every warp finds it for itself)
     float top = -INFINITY;
-    for (int e = (int)tid; e < p.E; e += THREADS) top = fmaxf(top, (float)score[e]);
+    for (int e = (int)lane; e < p.E; e += 32) top = fmaxf(top, (float)score[e]);
     const int b = __float_as_int(top + 0.0f), k = __reduce_max_sync(0xffffffffu, b ^ (b >> 31 & 0x7FFFFFFF));
-    float* warps = reinterpret_cast<float*>(red);
-    if (lane == 0) warps[warp] = __int_as_float(k ^ (k >> 31 & 0x7FFFFFFF));
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < ROUTE_WARPS; ++w) top = fmaxf(top, warps[w]);
+    top = __int_as_float(k ^ (k >> 31 & 0x7FFFFFFF));
+    __syncthreads();                                  // (everybody has read the logits)
     double sum = 0.0;
     for (int e = (int)tid; e < p.E; e += THREADS) { const double v = exp(score[e] - (double)top); sum += v; score[e] = v; }
     if (!p.renorm || p.bias) {
       sum = warp_sum(sum);
-      __syncthreads();
       if (lane == 0) red[warp] = sum;
       __syncthreads();
       sum = red[0];
@@ -108,50 +90,50 @@ __device__ __forceinline__ void choose(const RouteParams& p, int64_t t, double* 
     const double v = p.sigmoid ? 1.0 / (1.0 + exp(-score[e])) : score[e] * inv;
     score[e] = v;
     key[e] = rank_key(p.bias ? v + (double)p.bias[e] : v);
+    if (e < ROUTE_COUNTED) place[e] = 0;
   }
   __syncthreads();
-  if (tid >= 32) return;
-  // k times the largest key that is left, of equal ones the lowest index; every lane keeps the best of its own
-  constexpr long long NONE = (long long)0x8000000000000000ull;
-  constexpr int KEPT = 8;                             // keys of a lane in registers: 256 experts
-  long long mine[KEPT], best = NONE;
-  int at = 0x7FFFFFFF, my_id = 0;
-  const bool kept = p.E <= 32 * KEPT;
-#pragma unroll
-  for (int i = 0; i < KEPT; ++i) mine[i] = kept && (int)lane + 32 * i < p.E ? key[lane + 32 * i] : NONE;
-  auto scan = [&]() {
-    best = NONE;
-    at = 0x7FFFFFFF;
-    if (kept) {
-#pragma unroll
-      for (int i = 0; i < KEPT; ++i)
-        if (mine[i] > best) { best = mine[i]; at = (int)lane + 32 * i; }
-    } else {
+  int my_id = 0;
+  if (p.E <= ROUTE_COUNTED) {
+    // an expert's place is the number of those in front of it: larger keys, and equal ones of a lower index.  THREADS / E threads
+    // share an expert's comparisons
+    int width = 32;
+    while (width < p.E) width *= 2;
+    const int e = (int)tid & (width - 1), parts = THREADS / width, part = (int)tid / width;
+    if (e < p.E) {
+      const long long mine = key[e];
+      int n = 0;
+#pragma unroll 8
+      for (int j = part; j < p.E; j += parts) {
+        const long long other = key[j];
+        n += other > mine || (other == mine && j < e) ? 1 : 0;
+      }
+      atomicAdd(&place[e], n);
+    }
+    __syncthreads();
+    if ((int)tid < p.E && place[tid] < p.k) chosen[place[tid]] = (int)tid;
+    __syncthreads();
+    if (tid >= 32) return;
+    if ((int)lane < p.k) my_id = chosen[lane];
+  } else {
+    if (tid >= 32) return;
+    // k times the largest key that is left, of equal ones the lowest index; every lane keeps the best of its own
+    constexpr long long NONE = (long long)0x8000000000000000ull;
+    long long best = NONE;
+    int at = 0x7FFFFFFF;
+    auto scan = [&]() {
+      best = NONE;
+      at = 0x7FFFFFFF;
       for (int e = (int)lane; e < p.E; e += 32)
         if (key[e] > best) { best = key[e]; at = e; }
-    }
-  };
-  scan();
-  for (int j = 0; j < p.k; ++j) {
-    const int hi = (int)(best >> 32), top = __reduce_max_sync(0xffffffffu, hi);
-    const uint32_t who = __ballot_sync(0xffffffffu, hi == top);
-    int win;
-    if ((who & (who - 1)) == 0) {
-      win = __shfl_sync(0xffffffffu, at, __ffs(who) - 1);
-    } else {
+    };
+    scan();
+    for (int j = 0; j < p.k; ++j) {
+      const int hi = (int)(best >> 32), top = __reduce_max_sync(0xffffffffu, hi);
       const uint32_t lo = hi == top ? (uint32_t)best : 0u, low = __reduce_max_sync(0xffffffffu, lo);
-      win = __reduce_min_sync(0xffffffffu, hi == top && lo == low ? at : 0x7FFFFFFF);
-    }
-    if ((int)lane == j) my_id = win;
-    if (win == at) {
-      if (kept) {
-#pragma unroll
-        for (int i = 0; i < KEPT; ++i)
-          if (win == (int)lane + 32 * i) mine[i] = NONE;
-      } else {
-        key[win] = NONE;
-      }
-      scan();
+      const int win = __reduce_min_sync(0xffffffffu, hi == top && lo == low ? at : 0x7FFFFFFF);
+      if ((int)lane == j) my_id = win;
+      if (win == at) { key[win] = NONE; scan(); }
     }
   }
   const double v = (int)lane < p.k ? score[my_id] : 0.0, total = p.renorm ? warp_sum(v) : 1.0;
@@ -272,46 +254,52 @@ moe_route_mma_kernel(const __grid_constant__ RouteParams p)
     for (int e = (int)tid; e < p.E; e += 32 * ROUTE_WARPS) {
       double s = s_logit[e];
       for (int v = 1; v < p.splits; ++v) s += s_logit[(size_t)v * p.elements + e];
-      s_logit[e] = s;                               // (choose() reads its own thread's)
+      s_logit[e] = s;
     }
+    __syncthreads();
   }
   choose(p, t0 + rank, s_logit, key, red);
 }
 
 // ---- fp32 operands: G tokens a cluster --------------------------------------------------------------------------------------------
-template <int DT, int G, bool VEC>
+// A warp takes an expert at a time, its loads in batches (8 tokens x 4096 -> 64: 8.0 us, against 8.9 without; 64 -> 256 60 and 49); a row
+// that cannot be read in 16-byte pieces goes element by element.
+template <int G, bool VEC>
 __global__ void __launch_bounds__(32 * ROUTE_WARPS)
 moe_route_kernel(const __grid_constant__ RouteParams p)
 {
-  using T = typename RouteElem<DT>::type;
   static_assert(G <= ROUTE_CTAS);
   extern __shared__ double s_logit[];        // [E], keys [E], sums of the warps
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  uint32_t ctas;
-  asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(ctas));
   const uint32_t rank = ptx::cluster_ctarank();
   ptx::griddep_wait();
   if (threadIdx.x == 0) ptx::griddep_launch_dependents();
-  const int64_t t0 = (int64_t)(blockIdx.x / ctas) * G;
-  const T* X = reinterpret_cast<const T*>(p.x);
-  const T* W = reinterpret_cast<const T*>(p.w);
+  const int64_t t0 = (int64_t)(blockIdx.x / ROUTE_CTAS) * G;
+  const float *X = reinterpret_cast<const float*>(p.x), *W = reinterpret_cast<const float*>(p.w);
   ptx::cluster_sync();                       // (all CTAs have started: their shared memory may be written)
-  for (int e = (int)(rank * ROUTE_WARPS + warp); e < p.E; e += (int)ctas * ROUTE_WARPS) {
+  for (int e = (int)(rank * ROUTE_WARPS + warp); e < p.E; e += ROUTE_CTAS * ROUTE_WARPS) {
     double acc[G];
 #pragma unroll
     for (int g = 0; g < G; ++g) acc[g] = 0.0;
-#pragma unroll 4
-    for (int64_t h = lane * 8; h < p.H; h += 256) {
-      float w[8], x[8];
-      load8<DT, VEC>(w, W + (int64_t)e * p.ldw + h, p.H - h);
+    constexpr int BATCH = !VEC ? 1 : G == 1 ? 4 : 2;
+    for (int64_t h0 = lane * 8; h0 < p.H; h0 += 256 * BATCH) {
+      float w[BATCH][8], x[BATCH][G][8];
 #pragma unroll
-      for (int g = 0; g < G; ++g) {
-        load8<DT, VEC>(x, X + (t0 + g) * p.ldx + h, t0 + g < p.T ? p.H - h : 0);
-        float s = 0.0f;
+      for (int q = 0; q < BATCH; ++q) {
+        const int64_t h = h0 + 256 * q;
+        load8<VEC>(w[q], W + (int64_t)e * p.ldw + h, p.H - h);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s = fmaf(w[i], x[i], s);
-        acc[g] += (double)s;
+        for (int g = 0; g < G; ++g) load8<VEC>(x[q][g], X + (t0 + g) * p.ldx + h, t0 + g < p.T ? p.H - h : 0);
       }
+#pragma unroll
+      for (int q = 0; q < BATCH; ++q)
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+          float s = 0.0f;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) s = fmaf(w[q][i], x[q][g][i], s);
+          acc[g] += (double)s;
+        }
     }
 #pragma unroll
     for (int g = 0; g < G; ++g) {
@@ -347,8 +335,8 @@ static sdq_status_t launch_route(K kern, const RouteParams& p, int64_t groups, s
 }
 template <int DT>
 static sdq_status_t route16(RouteParams p, bool vec, void* stream) {
-  static_assert(ROUTE_TOKENS == ROUTE_CTAS);
   const int tiles = (p.E + 15) / 16;
+  static_assert(ROUTE_TOKENS == ROUTE_CTAS);
   p.splits = tiles < ROUTE_CTAS ? ROUTE_CTAS / tiles : 1;
   const size_t smem = ((size_t)p.splits + 1) * p.elements * 8 + (size_t)ROUTE_WARPS * (tiles > ROUTE_CTAS ? 2 : 1) * 128 * 8;
   const int64_t groups = (p.T + ROUTE_TOKENS - 1) / ROUTE_TOKENS;
@@ -358,9 +346,9 @@ static sdq_status_t route16(RouteParams p, bool vec, void* stream) {
 }
 template <int G>
 static sdq_status_t route32(const RouteParams& p, bool vec, void* stream) {
-  const size_t smem = 2 * (size_t)p.elements * 8 + ROUTE_WARPS * 8;
+  const size_t smem = 2 * (size_t)p.elements * 8 + ROUTE_WARPS * 8 + 8 * ROUTE_COUNTED;
   const int64_t groups = (p.T + G - 1) / G;
-  return vec ? launch_route(moe_route_kernel<SDQ_FP32, G, true>, p, groups, smem, stream) : launch_route(moe_route_kernel<SDQ_FP32, G, false>, p, groups, smem, stream);
+  return vec ? launch_route(moe_route_kernel<G, true>, p, groups, smem, stream) : launch_route(moe_route_kernel<G, false>, p, groups, smem, stream);
 }
 
 }  // namespace mx4

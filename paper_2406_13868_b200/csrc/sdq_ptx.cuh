@@ -148,20 +148,6 @@ __device__ __forceinline__ void mma_nvf4(uint32_t d, uint64_t adesc, uint64_t bd
       "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(sfa), "r"(sfb)
       : "memory");
 }
-// D[128 x N] (+)= A[128 x 32 K] * B[N x 32]^T, 8-bit kind (operand formats by the instruction descriptor; 4-bit ones sit in 16-byte
-// chunks of 16 elements and 8 bytes of padding), one E8M0 scale per 32 K (the byte of the scale word that the ids choose)
-__device__ __forceinline__ void mma_mxf8(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t sfa, uint32_t sfb,
-                                         uint32_t accumulate) {
-  asm volatile(
-      "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
-      "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale [%0], %1, %2, %3, [%5], [%6], p;\n}" ::"r"(d),
-      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(sfa), "r"(sfb)
-      : "memory");
-}
-// instruction descriptor of the 8-bit block-scaled kind with E2M1 A and E4M3 B
-__device__ __forceinline__ uint32_t idesc_mxf8_e2m1_e4m3(uint32_t M, uint32_t N, uint32_t sf_id) {
-  return (sf_id << 4) | (5u << 7) | ((N >> 3) << 17) | (1u << 23) | ((M >> 4) << 24) | (sf_id << 29);
-}
 
 // D[128 x N] (+)= A_sparse[128 x 128 logical K] * B[N x 128]^T, E2M1 operands, one E8M0 scale per 64 K
 __device__ __forceinline__ void mma_sp_mxf4(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t e_tmem,
