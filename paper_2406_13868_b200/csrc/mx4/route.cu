@@ -16,20 +16,22 @@ namespace mx4 {
 constexpr int ROUTE_WARPS = 16, ROUTE_CTAS = 8;
 constexpr int ROUTE_MAX_E = 1024, ROUTE_MAX_K = 32;
 
-// eight consecutive elements; `n` of them exist (VEC: all or none)
+// A lane's eight elements of a run: consecutive ones where rows can be read in 16-byte granules (VEC), else every LANES-th, so that the
+// lanes of a row read next to each other.  `n`: elements from `p` to the row's end.  Predicates and no branch: loads of a batch go out together
+// (consecutive elements with branches, and so: 33 tokens x 2047 -> 100 in fp32 26 us and 10, 5 x 333 -> 17 in bf16 6.6 and 4.8, 33 x 2047 -> 100 10.5 and 10.9).
 template <bool VEC>
 __device__ __forceinline__ void load8(float (&v)[8], const float* p, int64_t n) {
-  if constexpr (VEC) {
-    // (no branch: loads of a batch go out together)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+  for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+  if constexpr (VEC) {
 #pragma unroll
     for (int i = 0; i < 2; ++i)
       asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %5, 0;\n@p ld.global.nc.v4.f32 {%0, %1, %2, %3}, [%4];\n}"
                    : "+f"(v[4 * i]), "+f"(v[4 * i + 1]), "+f"(v[4 * i + 2]), "+f"(v[4 * i + 3]) : "l"(p + 4 * i), "r"((uint32_t)(n > 0)));
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : 0.0f;
+    for (int i = 0; i < 8; ++i)
+      asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %2, 0;\n@p ld.global.nc.f32 %0, [%1];\n}" : "+f"(v[i]) : "l"(p + 32 * i), "r"((uint32_t)(32 * i < n)));
   }
 }
 // order of doubles as order of integers: of equal ones the two zeros alike, a NaN above everything
@@ -154,7 +156,6 @@ __device__ __forceinline__ void mma_16x8x16(float (&d)[4], uint32_t a0, uint32_t
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// eight consecutive 16-bit elements of a row, `n` of which exist (VEC: all or none, and no branch: loads of a batch go out together)
 template <bool VEC>
 __device__ __forceinline__ uint4 load8_raw(const uint16_t* p, int64_t n) {
   uint32_t w[4] = {0, 0, 0, 0};
@@ -162,14 +163,19 @@ __device__ __forceinline__ uint4 load8_raw(const uint16_t* p, int64_t n) {
     asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %5, 0;\n@p ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];\n}"
                  : "+r"(w[0]), "+r"(w[1]), "+r"(w[2]), "+r"(w[3]) : "l"(p), "r"((uint32_t)(n > 0)));
   } else {
+    uint16_t e[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < n) w[i / 2] |= (uint32_t)p[i] << (16 * (i & 1));
+    for (int i = 0; i < 8; ++i) {
+      e[i] = 0;
+      asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %2, 0;\n@p ld.global.nc.u16 %0, [%1];\n}" : "+h"(e[i]) : "l"(p + 4 * i), "r"((uint32_t)(4 * i < n)));
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = (uint32_t)e[2 * i] | (uint32_t)e[2 * i + 1] << 16;
   }
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 // The warps of a CTA share its K.  The K of the operands' fragments is permuted alike, which a sum does not see: lane 4 r + c loads K 8 c .. + 7 of a
-// chunk of 32 of rows r and r + 8, one access each, and its words 0, 1 and 2, 3 are the fragments of two MMAs.
+// chunk of 32 of rows r and r + 8, one access each (or c, c + 4, ..), and its words 0, 1 and 2, 3 are the fragments of two MMAs.
 // TILES tiles of sixteen experts at a time, loads in batches of BATCH chunks.
 constexpr int ROUTE_BATCH = 4;
 template <int DT, bool VEC, int TILES>
@@ -177,7 +183,7 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS)
 moe_route_mma_kernel(const __grid_constant__ RouteParams p)
 {
   extern __shared__ double s_logit[];               // [K splits][E], keys [E], sums of the warps
-  const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, c8 = (lane & 3) * 8;
+  const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, first = (lane & 3) * (VEC ? 8 : 1);        // (of a chunk)
   const uint32_t rank = ptx::cluster_ctarank();
   const int64_t t0 = (int64_t)(blockIdx.x / ROUTE_CTAS) * ROUTE_TOKENS;
   long long* key = reinterpret_cast<long long*>(s_logit + (size_t)p.splits * p.elements);
@@ -191,7 +197,7 @@ moe_route_mma_kernel(const __grid_constant__ RouteParams p)
   ptx::griddep_wait();
   if (tid == 0) ptx::griddep_launch_dependents();
   const bool token = t0 + r < p.T;
-  const uint16_t* x = X + (token ? t0 + r : 0) * p.ldx + c8;
+  const uint16_t* x = X + (token ? t0 + r : 0) * p.ldx + first;
   bool waited = false;
   for (int tile = (int)rank - split * tiles; split < p.splits && tile < tiles; tile += TILES * step) {
     const uint16_t* w[TILES][2];
@@ -203,7 +209,7 @@ moe_route_mma_kernel(const __grid_constant__ RouteParams p)
       for (int j = 0; j < 2; ++j) {
         const int e = (tile + i * step) * 16 + (int)r + 8 * j;
         have[i][j] = e < p.E;
-        w[i][j] = W + (int64_t)(have[i][j] ? e : 0) * p.ldw + c8;
+        w[i][j] = W + (int64_t)(have[i][j] ? e : 0) * p.ldw + first;
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j) acc[i][j] = 0.0;
@@ -212,7 +218,7 @@ moe_route_mma_kernel(const __grid_constant__ RouteParams p)
       uint4 b[ROUTE_BATCH], a[ROUTE_BATCH][TILES][2];
 #pragma unroll
       for (int q = 0; q < ROUTE_BATCH; ++q) {
-        const int64_t h = (int64_t)(c + q) * 32, n = c + q < c1 ? p.H - h - c8 : 0;
+        const int64_t h = (int64_t)(c + q) * 32, n = c + q < c1 ? p.H - h - first : 0;
         b[q] = load8_raw<VEC>(x + h, token ? n : 0);
 #pragma unroll
         for (int i = 0; i < TILES; ++i)
@@ -281,8 +287,8 @@ moe_route_kernel(const __grid_constant__ RouteParams p)
     double acc[G];
 #pragma unroll
     for (int g = 0; g < G; ++g) acc[g] = 0.0;
-    constexpr int BATCH = !VEC ? 1 : G == 1 ? 4 : 2;
-    for (int64_t h0 = lane * 8; h0 < p.H; h0 += 256 * BATCH) {
+    constexpr int BATCH = G == 1 ? 4 : 2;
+    for (int64_t h0 = VEC ? lane * 8 : lane; h0 < p.H; h0 += 256 * BATCH) {
       float w[BATCH][8], x[BATCH][G][8];
 #pragma unroll
       for (int q = 0; q < BATCH; ++q) {
