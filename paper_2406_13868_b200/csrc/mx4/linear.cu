@@ -480,7 +480,7 @@ static cudaError_t with_smem(K kern, uint32_t bytes, DeviceInfo* d, int bit) {
   if (e == cudaSuccess) d->mx4_attr |= 1u << bit;
   return e;
 }
-constexpr uint32_t SMEM_MAX = 232448;
+constexpr uint32_t SMEM_MAX = 232448, NARROW_LEAST = 112640;
 
 // CTAs that share K of a row tile in the narrow kernel: as many as keep all of them resident, two an SM, with a tenth left over for clusters
 // that do not fit a GPU processing cluster (96 tiles x 3 of K = 4096 took 16.2 us, x 2 11.1); the sum over them is the dearer the more tokens there are
@@ -535,9 +535,12 @@ static sdq_status_t linear(GemmParams& p, DeviceInfo* d, void* stream) {
     if (parts > ring) p.nslot = (int32_t)((parts + slot - 1) / slot);
     lc.gridDim = dim3((unsigned)(p.n_tiles * ks), (unsigned)p.m_tiles);
     lc.blockDim = dim3(NARROW_THREADS);
-    // At least 80 KB: never more than two on an SM, as many as its tensor memory serves.  With a third, CTAs of two clusters could each hold
-    // the columns that the other's peer waits for
-    lc.dynamicSmemBytes = (uint32_t)p.nslot * slot + NARROW_TAIL > 81920u ? (uint32_t)p.nslot * slot + NARROW_TAIL : 81920u;
+    // At least nearly half of an SM's (what two leave is for the next launch's small kernel): columns of tensor memory then always suffice for all
+    // that an SM has room for (256 here; the library's other products take 512 with more than half of the shared memory, 256 with half, or 128
+    // and run two an SM).  Beyond that, CTAs of two clusters could each hold the columns that the other's peer waits for, and a kernel in front
+    // that lets this one in before it has its own would wait for this one, which waits for it
+    const uint32_t bytes = (uint32_t)p.nslot * slot + NARROW_TAIL;
+    lc.dynamicSmemBytes = bytes > NARROW_LEAST ? bytes : NARROW_LEAST;
     attr[1].val.clusterDim.x = (unsigned)ks;
     p.wide_rows = ((uintptr_t)p.Y % (4 * dtype_bytes(DT))) == 0 && (p.ldy % 4 == 0 || p.M == 1);
     auto kern = mx4_linear_narrow_kernel<FMT, DT>;
@@ -554,8 +557,8 @@ static sdq_status_t linear(GemmParams& p, DeviceInfo* d, void* stream) {
     constexpr bool V = decltype(v)::value;
     constexpr uint32_t bytes = wide_slots(FMT, V) * wide_slot(FMT) + wide_tail(V);
     static_assert(bytes <= SMEM_MAX, "the ring fits");
-    lc.dynamicSmemBytes = bytes;
-    if (with_smem(kern, bytes, d, bit) != cudaSuccess) return launch_status(cudaErrorUnknown);
+    lc.dynamicSmemBytes = SMEM_MAX;                  // (an SM's: nothing else that takes tensor memory is beside it)
+    if (with_smem(kern, SMEM_MAX, d, bit) != cudaSuccess) return launch_status(cudaErrorUnknown);
     return launch_status(cudaLaunchKernelEx(&lc, kern, p));
   };
   return vec ? go(mx4_linear_wide_kernel<FMT, DT, true>, std::true_type{}, BIT + 1) : go(mx4_linear_wide_kernel<FMT, DT, false>, std::false_type{}, BIT + 2);

@@ -697,7 +697,7 @@ static sdq_status_t moe(MoeParams p, DeviceInfo* d, void* stream) {
   }
   {
     // two CTAs an SM, twice as many as SMs where there is work for them: an SM's two MMA issuers hide each other's trips, and the SMs that
-    // have one CTA get the more of the memory's bandwidth (128 CTAs, one an SM: ..)
+    // have one CTA get the more of the memory's bandwidth (64 tokens, 2 of 8 experts of 4096 x 11008: the layer 147 us with one an SM, 130 with two)
     p.tmem_cols = 256;
     int ks = 1;
     while (ks < 8 && 2 * ks * p.tiles_h <= 2 * d->sm_count && 2 * ks <= p.max_units * p.off.si) ks *= 2;

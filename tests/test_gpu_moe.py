@@ -65,6 +65,20 @@ def test_route_ties_take_the_lowest_index(m):
     assert torch.allclose(weights.sum(1), torch.ones(3, device="cuda")) and (weights[2] == 0.125).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("T,E,k", [(9, 2, 2), (3, 31, 31), (8, 33, 32), (17, 127, 9), (5, 128, 32), (5, 129, 32), (2, 1000, 32)])
+def test_route_order_of_many_ties(m, dtype, T, E, k):
+    """logits that are exact small integers: of equal ones the lowest index, up to the number of experts where places are counted and beyond"""
+    g = torch.Generator().manual_seed(T + E)
+    x, w = (torch.randint(-1, 2, s, generator=g).to(DT[dtype]) for s in ((T, 20), (E, 20)))
+    ids, weights = m.sdq_moe_route(x.cuda(), w.cuda(), k, renorm=False)
+    logits = x.double() @ w.double().T
+    want = torch.sort(logits, dim=1, descending=True, stable=True)[1][:, :k]
+    assert torch.equal(ids.cpu().long(), want)
+    score = torch.softmax(logits, 1).gather(1, want)
+    assert ((weights.cpu().double() - score).abs() <= 2.0 ** -23 * score).all()      # (64-bit scores, rounded once)
+
+
 @pytest.mark.parametrize("H", [64, 65])
 def test_route_strides_and_non_finite_tokens(m, H):
     g = torch.Generator().manual_seed(1)

@@ -38,7 +38,25 @@ def test_every_kernel_lets_the_next_launch_in_behind_its_own_wait(bodies):
     for n, b in bodies.items():
         lets_in = [x.start() for x in re.finditer(r"griddep_launch_dependents\(\)", b)]
         assert len(lets_in) == 1, n
-        assert re.search(r"ptx::griddep_wait\(\);\s*if \((?:lane|tid|threadIdx\.x) == 0\) $", b[:lets_in[0] - len("ptx::")]), n
+        waits = [x.start() for x in re.finditer(r"ptx::griddep_wait\(\);", b[:lets_in[0]])]
+        assert waits and "else if (warp" not in b[waits[-1]:lets_in[0]], n          # (by a thread that has waited itself)
+
+
+def test_tensor_memory_is_taken_before_the_next_launch_is_let_in(bodies):
+    """else the next launch could take the columns and wait for this one, which waits for them"""
+    for n, b in bodies.items():
+        if "tmem_alloc" in b:
+            assert b.index("tmem_alloc") < b.index("griddep_launch_dependents()"), n
+
+
+def test_a_products_columns_of_tensor_memory_suffice_for_what_an_sm_has_room_for():
+    """256 columns come with nearly half of an SM's shared memory (1 KB of it reserved for each CTA): two leave less than any product's
+    smallest ring (16 KB) takes"""
+    src, moe = (open(os.path.join(MX4, n)).read() for n in ("linear.cu", "moe.cu"))
+    assert "lc.dynamicSmemBytes = bytes > NARROW_LEAST ? bytes : NARROW_LEAST;" in src and "lc.dynamicSmemBytes = SMEM_MAX;" in src
+    least = int(re.search(r"NARROW_LEAST = (\d+);", src).group(1))
+    assert 0 < 233472 - 2 * (least + 1024) < 15000
+    assert "const uint32_t room = (half ? SMEM_MAX / 2 - 1024 : SMEM_MAX) - 1024 - 128;" in moe
 
 
 def test_global_memory_is_read_behind_the_wait_for_the_launch_in_front(bodies):
