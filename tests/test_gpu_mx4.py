@@ -289,3 +289,37 @@ def test_many_long_rows_are_quantized_like_few(m, dtype, R, K, pad):
     check = x[:40].cpu()
     check_quantized(m, m.sdq_mx4_quantize(x[:40], m.FMT_NVFP4), check, True, False)
     assert m.device_status() == 0
+
+
+def test_beside_the_decomposed_layers(m):
+    """both kinds of products one behind the other in a stream, and in two streams at once, give what each gives alone"""
+    K, N = 1024, 1280
+    g = torch.Generator().manual_seed(21)
+    W = (torch.randn(N, K, generator=g) * 0.02).bfloat16().cuda()
+    cfg = m.Config(out_n=1, in_gran=m.GRAN_PAIR, in_block=64, scale_rule=m.SCALE_OCP_FLOOR)
+    P, Q = m.sdq_decompose(W, cfg), m.sdq_mx4_quantize(W, m.FMT_NVFP4)
+    for M in (2, 40, 128, 300):
+        X = torch.randn(M, K, generator=g).bfloat16().cuda()
+
+        def old():
+            return m.sdq_linear(m.sdq_quantize_act(X, cfg), P)
+
+        def new():
+            return m.sdq_mx4_linear(m.sdq_mx4_quantize(X, m.FMT_NVFP4), Q)
+
+        torch.cuda.synchronize()
+        a = old()
+        torch.cuda.synchronize()
+        b = new()
+        torch.cuda.synchronize()
+        xa, xb = m.sdq_quantize_act(X, cfg), m.sdq_mx4_quantize(X, m.FMT_NVFP4)
+        turns = [f() for _ in range(10) for f in (old, new, lambda: m.sdq_linear(xa, P), lambda: m.sdq_mx4_linear(xb, Q))]
+        streams = [torch.cuda.Stream() for _ in range(2)]
+        torch.cuda.synchronize()
+        for i in range(20):
+            for s, f in zip(streams, (old, new)):
+                with torch.cuda.stream(s):
+                    turns.append(f())
+        torch.cuda.synchronize()
+        assert all(torch.equal(y, b if i % 2 else a) for i, y in enumerate(turns))
+    assert m.device_status() == 0
