@@ -668,8 +668,8 @@ static sdq_status_t moe(MoeParams p, DeviceInfo* d, void* stream) {
   const int pairs = p.T * p.k;
   p.unit = unit_pairs(p.T);
   p.max_units = (pairs < p.E ? pairs : p.E) + pairs / p.unit;
-  // Few tokens: both products in half an SM's shared and tensor memory, so that the second's CTAs run beside the first's and have their weights
-  // under way when h comes.  More than 76 KB each in any case: never a third such CTA on an SM, which tensor memory would not serve
+  // Few tokens: both products in half an SM's shared and tensor memory, so that two CTAs of the first run on an SM, or the second's CTAs beside the
+  // first's, with their weights under way when h comes.  More than 76 KB each in any case: never a third such CTA on an SM, which tensor memory would not serve
   const bool half = p.T <= 16;
   p.tmem_cols = half ? 256 : 512;
   const uint32_t room = (half ? SMEM_MAX / 2 - 1024 : SMEM_MAX) - 1024 - 128;
@@ -682,15 +682,19 @@ static sdq_status_t moe(MoeParams p, DeviceInfo* d, void* stream) {
   }
   {
     const int64_t tasks = (int64_t)p.max_units * p.tiles_i;                // (at most)
+    // (half an SM each and more tasks than SMs: two CTAs an SM, as in the second product.  us with one and with two: 16 tokens, 8 of 64 experts of
+    // 4096 x 1408, 146 and 127, 8 tokens, 2 of 8 of 4096 x 11008, 117 and 108, 1 token, 2 of 8 of 4096 x 14336, 53.6 and 48.3, 3 tokens, 2 of 35 of
+    // 2899 x 3121, 36.7 and 32.2)
+    const int64_t at_once = half && tasks > d->sm_count ? 2 * d->sm_count : d->sm_count;
     int best = 1;
     int64_t cost = 0;
     for (int ks = 1; ks <= 8 && ks <= p.off.sh; ks *= 2) {
-      const int64_t cl = d->sm_count / ks, c = ((tasks + cl - 1) / cl) * ((p.off.sh + ks - 1) / ks + (ks > 1 ? 4 : 2));
+      const int64_t cl = at_once / ks, c = ((tasks + cl - 1) / cl) * ((p.off.sh + ks - 1) / ks + (ks > 1 ? 4 : 2));
       if (ks == 1 || c < cost) { best = ks; cost = c; }
     }
     const uint32_t behind = (uint32_t)p.unit * 1024u + (uint32_t)p.max_units * (uint32_t)sizeof(MoeUnit);
     p.ring_bytes = (int32_t)((room - behind) / 128 * 128);
-    const int64_t cl = d->sm_count / best < tasks ? d->sm_count / best : tasks;
+    const int64_t cl = at_once / best < tasks ? at_once / best : tasks;
     Launch l((unsigned)(cl * best), MOE_THREADS, (unsigned)best, (size_t)p.ring_bytes + behind + 128, stream);
     const sdq_status_t st = launch_status(cudaLaunchKernelEx(&l.lc, up, p));
     if (st != SDQ_OK) return st;
