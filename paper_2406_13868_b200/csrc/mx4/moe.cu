@@ -33,7 +33,9 @@ constexpr int MOE_MAX_T = 64, MOE_MAX_K = 32, MOE_MAX_E = 1024;
 constexpr int PIECES = 6;
 // Pairs of a unit, at most: six pieces of 20 are 120 columns, which one scale atom serves.  Smaller units where there are fewer tokens bound
 // what a CTA has to have room for; a token may name an expert more than once, so that the number of tokens alone bounds nothing.
-__host__ __device__ constexpr int unit_pairs(int64_t T) { return T <= 8 ? 8 : T <= 16 ? 16 : 20; }
+// (A unit's pieces are whole groups of eight rows: a multiple of four pairs.)  Sixteen where an expert has eight pairs or fewer in the mean, and so
+// seldom more than sixteen
+constexpr int unit_pairs(int64_t T, int64_t pairs, int64_t E) { return T <= 8 ? 8 : T <= 16 || pairs <= 8 * E ? 16 : 20; }
 
 // ---- workspace --------------------------------------------------------------------------------------------------------------
 struct MoeUnit { int32_t expert, n, pair0, group; };        // pairs pair0 .. + n of the sorted list; first 8-row group of its pieces
@@ -666,25 +668,26 @@ static sdq_status_t moe(MoeParams p, DeviceInfo* d, void* stream) {
   auto down = moe_down_kernel<DT>;
   if (!with_smem(up, d, 0) || !with_smem(down, d, 1 + DT)) return launch_status(cudaErrorUnknown);
   const int pairs = p.T * p.k;
-  p.unit = unit_pairs(p.T);
+  p.unit = unit_pairs(p.T, pairs, p.E);
   p.max_units = (pairs < p.E ? pairs : p.E) + pairs / p.unit;
-  // Few tokens: both products in half an SM's shared and tensor memory, so that two CTAs of the first run on an SM, or the second's CTAs beside the
+  // Few pairs an expert: both products in half an SM's shared and tensor memory, so that two CTAs of the first run on an SM, or the second's CTAs beside the
   // first's, with their weights under way when h comes.  More than 76 KB each in any case: never a third such CTA on an SM, which tensor memory would not serve
-  const bool half = p.T <= 16;
+  const bool half = p.unit <= 16, few = p.T <= 16;
   p.tmem_cols = half ? 256 : 512;
   const uint32_t room = (half ? SMEM_MAX / 2 - 1024 : SMEM_MAX) - 1024 - 128;
   {
     const size_t smem = (size_t)(pairs + 3) / 4 * 4 * 8 + (size_t)p.E * 16;
-    const int threads = half ? 64 : 256;
+    const int threads = few ? 64 : 256;
     Launch l((unsigned)((p.T * 16 * (int64_t)p.off.sh + threads - 1) / threads), (unsigned)threads, 0, smem, stream);
-    const sdq_status_t st = launch_status(half ? cudaLaunchKernelEx(&l.lc, moe_split_kernel<DT, 64>, p) : cudaLaunchKernelEx(&l.lc, moe_split_kernel<DT, 256>, p));
+    const sdq_status_t st = launch_status(few ? cudaLaunchKernelEx(&l.lc, moe_split_kernel<DT, 64>, p) : cudaLaunchKernelEx(&l.lc, moe_split_kernel<DT, 256>, p));
     if (st != SDQ_OK) return st;
   }
   {
     const int64_t tasks = (int64_t)p.max_units * p.tiles_i;                // (at most)
     // (half an SM each and more tasks than SMs: two CTAs an SM, as in the second product.  us with one and with two: 16 tokens, 8 of 64 experts of
     // 4096 x 1408, 146 and 127, 8 tokens, 2 of 8 of 4096 x 11008, 117 and 108, 1 token, 2 of 8 of 4096 x 14336, 53.6 and 48.3, 3 tokens, 2 of 35 of
-    // 2899 x 3121, 36.7 and 32.2)
+    // 2899 x 3121, 36.7 and 32.2; 32 tokens, 2 of 8 of 4096 x 11008, in units of twenty by one CTA 119, of sixteen by two 108, 17 tokens,
+    // 8 of 64 of 4096 x 1408, 142 and 121)
     const int64_t at_once = half && tasks > d->sm_count ? 2 * d->sm_count : d->sm_count;
     int best = 1;
     int64_t cost = 0;

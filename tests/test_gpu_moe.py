@@ -166,6 +166,9 @@ def test_moe_one_expert_for_everybody(m):
     """more pairs than one unit takes, among them a token that names an expert eight times"""
     check_moe(m, 64, 140, 150, 6, 2, "bf16", ids=torch.tensor([[3, 5]] * 63 + [[3, 3]]))
     check_moe(m, 20, 140, 150, 6, 8, "fp16", ids=torch.full((20, 8), 2))
+    # (units of sixteen, for few pairs an expert in the mean)
+    check_moe(m, 40, 300, 290, 32, 3, "bf16", ids=torch.tensor([[7, 31, 7]] * 25 + [[7, 0, 12]] * 15))
+    check_moe(m, 64, 140, 1300, 20, 2, "bf16", ids=torch.tensor([[t % 20, 17] for t in range(64)]))
 
 
 @pytest.mark.parametrize("H", [256, 250])
