@@ -49,6 +49,23 @@ template <int DT> __device__ __forceinline__ float from_out(typename Out<DT>::ty
   else return v;
 }
 
+// ---- row factors (NVFP4) ----------------------------------------------------------------------------------------------------
+// s fw fx + b.  The product of two factors that both lie in [2^-62, 2^62], or are zero, is a normal number or zero: one multiplication of the sum.
+// Others, a whole row's magnitude each, can leave fp32's range together although the output does not, and are applied one after the other: where
+// their product is too small the larger one first, where it is too large the smaller one.  s is zero or between 2^-20, the smallest product of two held elements, and 2^53,
+// so that nothing in between is lost: factors of a product below 2^-126 have a larger one of at most 2^23 (the smaller one is 2^-149 or more), and s
+// times it is a subnormal number only where the output is zero; of a product above 2^128, a smaller one above 1, and s times it is too large only
+// where the output is.
+__device__ __forceinline__ bool plain_factor(float f) {
+  const uint32_t e = __float_as_uint(f) << 1;
+  return e == 0u || (e >= (65u << 24) && e <= (189u << 24));
+}
+__device__ __forceinline__ float apply_factors(float s, float fw, float fx, float b) {
+  const float f = fw * fx, mag = fabsf(f), large = fabsf(fw) > fabsf(fx) ? fw : fx, small = fabsf(fw) > fabsf(fx) ? fx : fw;
+  if (mag >= 1.17549435e-38f && mag < INFINITY) return fmaf(s, f, b);
+  return mag < 1.0f ? fmaf(s * large, small, b) : fmaf(s * small, large, b);      // (a NaN stays one)
+}
+
 // ---- few tokens -----------------------------------------------------------------------------------------------------------
 constexpr int NARROW_THREADS = 256;                  // weights' producer, MMA issuer, tokens' producer, an idle warp, four epilogue warps
 constexpr uint32_t NARROW_TAIL = 256 + 128;          // barriers, and room to align the ring to 128 bytes
@@ -180,10 +197,12 @@ mx4_linear_narrow_kernel(const __grid_constant__ GemmParams p)
     const int64_t n0 = (int64_t)nt * ROWS, m0 = (int64_t)mt * 128;
     const uint32_t n = (tid & 31u) * 4;                          // this thread's rows of the tile
     float fw[4], b[4];
+    bool plain_w = true;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const bool in = n0 + n + j < p.N;
       fw[j] = FMT == SDQ_FMT_NVFP4 && in ? p.fw[n0 + n + j] : 1.0f;
+      plain_w = plain_w && plain_factor(fw[j]);
       b[j] = p.bias && in ? from_out<DT>(reinterpret_cast<const T_out*>(p.bias)[n0 + n + j]) : 0.0f;
     }
     const int valid = (int)min((int64_t)T, p.M - m0);
@@ -195,8 +214,13 @@ mx4_linear_narrow_kernel(const __grid_constant__ GemmParams p)
       const float fx = FMT == SDQ_FMT_NVFP4 ? __ldg(p.fx + m0 + c) : 1.0f;
       const float s[4] = {s4.x, s4.y, s4.z, s4.w};
       T_out o[4];
+      if (FMT != SDQ_FMT_NVFP4 || (plain_w && plain_factor(fx))) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) o[j] = to_out<DT>(fmaf(s[j], FMT == SDQ_FMT_NVFP4 ? fw[j] * fx : 1.0f, b[j]));
+        for (int j = 0; j < 4; ++j) o[j] = to_out<DT>(fmaf(s[j], FMT == SDQ_FMT_NVFP4 ? fw[j] * fx : 1.0f, b[j]));
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] = to_out<DT>(apply_factors(s[j], fw[j], fx, b[j]));
+      }
       T_out* y = reinterpret_cast<T_out*>(p.Y) + (m0 + c) * p.ldy + n0 + n;
       if (whole) {
         if constexpr (DT == SDQ_FP32) *reinterpret_cast<float4*>(y) = make_float4(o[0], o[1], o[2], o[3]);
@@ -393,7 +417,10 @@ mx4_linear_wide_kernel(const __grid_constant__ GemmParams p)
       const int64_t m = (int64_t)(2 * mt + (int)rank) * ROWS + q * 32 + lane;
       const float fx = FMT == SDQ_FMT_NVFP4 && m < p.M ? __ldg(p.fx + m) : 1.0f;
       if (et == 0 && !ptx::mbar_wait(acc_full, (uint32_t)t & 1u)) *timed_out = 1u;
-      ptx::named_bar_sync(1, 256);
+      // (whether all factors of the CTA's tile are plain ones comes with the barrier)
+      bool plain = true;
+      if constexpr (FMT == SDQ_FMT_NVFP4) plain = ptx::named_bar_all(1, 256, plain_factor(fac[et]) && plain_factor(fx));
+      else ptx::named_bar_sync(1, 256);
       if (*timed_out) { ok = false; break; }
       ptx::tc_fence_after();
       // (four-byte outputs in two parts: what a thread holds is 64 words)
@@ -408,10 +435,18 @@ mx4_linear_wide_kernel(const __grid_constant__ GemmParams p)
           uint32_t v[16];
           ptx::tmem_ld_32x32b_x16(tmem + ((q * 32u) << 16) + c0 + 16u * c, v);
           ptx::tmem_ld_wait();
+          if (plain) {
 #pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            const uint32_t col = c0 + 16u * c + j;
-            v[j] = __float_as_uint(fmaf(__uint_as_float(v[j]), FMT == SDQ_FMT_NVFP4 ? fac[col] * fx : 1.0f, fac[256 + col]));
+            for (int j = 0; j < 16; ++j) {
+              const uint32_t col = c0 + 16u * c + j;
+              v[j] = __float_as_uint(fmaf(__uint_as_float(v[j]), FMT == SDQ_FMT_NVFP4 ? fac[col] * fx : 1.0f, fac[256 + col]));
+            }
+          } else {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              const uint32_t col = c0 + 16u * c + j;
+              v[j] = __float_as_uint(apply_factors(__uint_as_float(v[j]), fac[col], fx, fac[256 + col]));
+            }
           }
 #pragma unroll
           for (int j = 0; j < 16 / PER; ++j) {

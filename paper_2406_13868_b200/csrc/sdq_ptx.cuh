@@ -362,6 +362,13 @@ __device__ __forceinline__ float4 ld_cluster_f32x4(uint32_t raddr) {
 __device__ __forceinline__ void named_bar_sync(uint32_t id, uint32_t threads) {
   asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
 }
+// the same; whether `x` holds for every thread
+__device__ __forceinline__ bool named_bar_all(uint32_t id, uint32_t threads, bool x) {
+  uint32_t all;
+  asm volatile("{\n.reg .pred p, q;\nsetp.ne.u32 p, %3, 0;\nbarrier.cta.red.and.pred q, %1, %2, p;\nselp.u32 %0, 1, 0, q;\n}"
+               : "=r"(all) : "r"(id), "r"(threads), "r"((uint32_t)x) : "memory");
+  return all != 0;
+}
 // this warp's arrival on a named barrier that others wait on
 __device__ __forceinline__ void named_bar_arrive(uint32_t id, uint32_t threads) {
   asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory");
