@@ -70,6 +70,12 @@ sdq_status_t sdq_diag_linear_rings(int64_t M, int64_t N, int64_t K, const sdq_co
 sdq_status_t sdq_diag_group_plan(int n, int64_t M, const int64_t* N, const int64_t* K, int sm_count, const int* max_clusters,
                                  sdq_diag_plan_t* out, sdq_diag_task_t* segs, int64_t cap);
 
+/* How an NVFP4 quantizer call (sdq_mx4_quantize of R rows of K elements of `dtype`, at a device address of which only the alignment counts) goes
+ * through its rows: *rows of them at a time through *buffers buffers of *shared bytes of shared memory in all; all zero where the
+ * call runs a form without such buffers.  Host code only.  Errors: INVALID_ARG, SHAPE. */
+sdq_status_t sdq_diag_mx4_quantize_rows(uint64_t address, int64_t R, int64_t K, int64_t ldx, int32_t dtype, int32_t* rows, int32_t* buffers,
+                                        int64_t* shared);
+
 #ifdef __cplusplus
 }
 #endif

@@ -8,6 +8,7 @@
 
 #include <type_traits>
 
+#include "../../../include/sdq_diag.h"
 #include "../sdq_codec.cuh"
 #include "../sdq_internal.h"
 #include "layout.h"
@@ -726,6 +727,21 @@ template <typename... P, typename... A>
 static sdq_status_t launch(void (*kern)(P...), dim3 grid, unsigned threads, void* stream, A... args) { return launch_as(0, 0, kern, grid, threads, stream, args...); }
 constexpr int NS_SMEM = 227328;              // (beside the kernel's own)
 constexpr int64_t NS_FROM = 1 << 22;          // elements from which rows are streamed
+// Whether the rows of an NVFP4 matrix of a 16-bit type are streamed through shared memory (rows of a turn; 0: they are not), and in how many
+// buffers: rows in 16-byte granules, more than one unit a warp in the cluster form, 2^22 elements of them at least, and two buffers that fit.
+// (Rows may have 2^31 bytes: compared in 64 bits.)
+struct StreamForm {
+  int rows, buffers;
+  uint32_t row_bytes;
+  size_t shared() const { return (size_t)rows * (size_t)buffers * row_bytes; }
+};
+static StreamForm stream_form(uintptr_t X, int64_t R, int64_t K, int64_t ld, int dtype) {
+  const int64_t es = (int64_t)dtype_bytes(dtype), per = 16 / es, row_bytes = K * es, units = (K + KREC - 1) / KREC * (KREC / UNIT_K);
+  if (dtype == SDQ_FP32 || (X & 15) || K % per || ld % per || units <= NV_CTAS * Q_WARPS || row_bytes > NS_SMEM / 4 || R < (NS_FROM + K - 1) / K) return {0, 0, 0};
+  const int rows = row_bytes <= NS_SMEM / 8 ? 4 : 2;
+  const int64_t buffers = NS_SMEM / (row_bytes * rows);
+  return {rows, buffers < NS_MAX_BUFFERS ? (int)buffers : NS_MAX_BUFFERS, (uint32_t)row_bytes};
+}
 // 8-row groups, one a thread block along x: linear: those that hold rows; experts: of all padded rows
 static int64_t groups_of(int64_t E, const Shape& s) { return E ? E * s.tiles * 16 : (s.R + 7) / 8; }
 static unsigned blocks_along_k(const Shape& s, int warps) { return (unsigned)((s.units + warps - 1) / warps < 65535 ? (s.units + warps - 1) / warps : 65535); }
@@ -747,27 +763,22 @@ static sdq_status_t quantize(const void* X, int64_t E, const Shape& s, int fmt, 
   const int64_t groups = groups_of(E, s);
   if (groups > 0x7FFFFFFF) return SDQ_ERR_SHAPE;
   if (fmt == SDQ_FMT_NVFP4) {
-    // rows in 16-byte granules, more than one unit a warp in the cluster form, 2^22 elements of them at least, and two buffers that fit
-    const uint32_t row_bytes = (uint32_t)((s.K * (int64_t)sizeof(T) + 15) / 16 * 16);
-    const int64_t per = 16 / (int64_t)sizeof(T);
     DeviceInfo* d = device_info();
     uint32_t* flags = device_flags();
     if (!d || !flags) return SDQ_ERR_CUDA;
     if constexpr (DT != SDQ_FP32) {
-      if (((uintptr_t)X & 15) == 0 && s.K % per == 0 && s.ld % per == 0 && s.units > NV_CTAS * Q_WARPS && row_bytes * 4u <= NS_SMEM && s.R * s.K >= NS_FROM) {
-        auto stream_rows = [&](auto kern, int rb, int bit) {
+      const StreamForm f = stream_form((uintptr_t)X, s.R, s.K, s.ld, DT);
+      if (f.rows) {
+        auto stream_rows = [&](auto kern, int bit) {
           if (!(d->mx4_quant_attr & (1u << bit))) {
             if (cudaFuncSetAttribute((const void*)kern, cudaFuncAttributeMaxDynamicSharedMemorySize, NS_SMEM) != cudaSuccess) return launch_status(cudaErrorUnknown);
             d->mx4_quant_attr |= 1u << bit;
           }
-          int buffers = NS_SMEM / (int)(row_bytes * (uint32_t)rb);
-          if (buffers > NS_MAX_BUFFERS) buffers = NS_MAX_BUFFERS;
-          const int64_t blocks = (s.R + rb - 1) / rb;
-          return launch_as(0, (size_t)buffers * rb * row_bytes, kern, dim3((unsigned)(blocks < d->sm_count ? blocks : d->sm_count)), 32 * NS_WARPS, stream, x, s, buffers, row_bytes,
+          const int64_t blocks = (s.R + f.rows - 1) / f.rows;
+          return launch_as(0, f.shared(), kern, dim3((unsigned)(blocks < d->sm_count ? blocks : d->sm_count)), 32 * NS_WARPS, stream, x, s, f.buffers, f.row_bytes,
                            buf, flags);
         };
-        if (row_bytes * 8u <= NS_SMEM) return stream_rows(nv4_quantize_stream_kernel<DT, 4>, 4, 2 * DT);
-        return stream_rows(nv4_quantize_stream_kernel<DT, 2>, 2, 2 * DT + 1);
+        return f.rows == 4 ? stream_rows(nv4_quantize_stream_kernel<DT, 4>, 2 * DT) : stream_rows(nv4_quantize_stream_kernel<DT, 2>, 2 * DT + 1);
       }
     }
     // one unit a warp where the CTAs of a cluster have as many warps, else two; short rows take fewer warps
@@ -891,4 +902,13 @@ extern "C" sdq_status_t sdq_mx4_dequantize(const sdq_mx4_t* q, void* out, int32_
   return dtype == SDQ_BF16   ? mx4::dequantize<SDQ_BF16>(q, out, ldo, stream)
          : dtype == SDQ_FP16 ? mx4::dequantize<SDQ_FP16>(q, out, ldo, stream)
                              : mx4::dequantize<SDQ_FP32>(q, out, ldo, stream);
+}
+
+extern "C" sdq_status_t sdq_diag_mx4_quantize_rows(uint64_t address, int64_t R, int64_t K, int64_t ldx, int32_t dtype, int32_t* rows, int32_t* buffers, int64_t* shared)
+{
+  if (!rows || !buffers || !shared || !mx4::dtype_ok(dtype)) return SDQ_ERR_INVALID_ARG;
+  if (!mx4::size_ok(0, R, K) || ldx < K) return SDQ_ERR_SHAPE;
+  const mx4::StreamForm f = mx4::stream_form((uintptr_t)address, R, K, ldx, dtype);
+  *rows = f.rows; *buffers = f.buffers; *shared = (int64_t)f.shared();
+  return SDQ_OK;
 }
