@@ -67,6 +67,12 @@ sdq_status_t sdq_diag_linear_plan(int64_t M, int64_t N, int64_t K, const sdq_con
 typedef struct { int32_t slots, slot_bytes, out_slots, out_slot_bytes, bytes; } sdq_diag_rings_t;
 sdq_status_t sdq_diag_linear_rings(int64_t M, int64_t N, int64_t K, const sdq_config_t* cfg, int sm_count, const int* max_clusters,
                                    sdq_diag_rings_t* out);
+/* What a thread block of such a call takes of an SM: dynamic shared memory in bytes (1 KB more is reserved for each) and columns of tensor memory.
+ * sdq_diag_group_memory: of the grouped kernel, M (up to 32) tokens of K channels, layers with out_n outliers per S-Vector; activations != 0: with
+ * the activations quantized inside (sdq_linear_group_x). */
+sdq_status_t sdq_diag_linear_memory(int64_t M, int64_t N, int64_t K, const sdq_config_t* cfg, int workspace, int sm_count, const int* max_clusters,
+                                    int32_t* shared, int32_t* columns);
+sdq_status_t sdq_diag_group_memory(int64_t M, int64_t K, int out_n, int activations, int32_t* shared, int32_t* columns);
 sdq_status_t sdq_diag_group_plan(int n, int64_t M, const int64_t* N, const int64_t* K, int sm_count, const int* max_clusters,
                                  sdq_diag_plan_t* out, sdq_diag_task_t* segs, int64_t cap);
 

@@ -79,7 +79,7 @@ EXPORTS = ["sdq_packed_size", "sdq_decompose", "sdq_decompose_metric", "sdq_chan
            "sdq_linear", "sdq_linear_f32", "sdq_workspace_size", "sdq_workspace_init", "sdq_linear_ws", "sdq_linear_f32_ws", "sdq_linear_noalloc",
            "sdq_linear_group", "sdq_linear_group_f32", "sdq_linear_group_x", "sdq_linear_group_x_f32", "sdq_linear_group_x_ws", "sdq_linear_group_x_f32_ws", "sdq_mx4_size", "sdq_mx4_quantize", "sdq_mx4_import", "sdq_mx4_export", "sdq_mx4_dequantize", "sdq_mx4_linear",
            "sdq_mx4_experts_size", "sdq_mx4_experts_quantize", "sdq_mx4_experts_import",
-           "sdq_moe_route", "sdq_mx4_moe_workspace_size", "sdq_mx4_moe", "sdq_diag_l2_copy", "sdq_diag_wait_timeout", "sdq_diag_decompose_timeout", "sdq_diag_linear_plan", "sdq_diag_linear_rings", "sdq_diag_group_plan", "sdq_diag_mx4_quantize_rows", "sdq_device_status", "sdq_status_string"]
+           "sdq_moe_route", "sdq_mx4_moe_workspace_size", "sdq_mx4_moe", "sdq_diag_l2_copy", "sdq_diag_wait_timeout", "sdq_diag_decompose_timeout", "sdq_diag_linear_plan", "sdq_diag_linear_rings", "sdq_diag_group_plan", "sdq_diag_linear_memory", "sdq_diag_group_memory", "sdq_diag_mx4_quantize_rows", "sdq_device_status", "sdq_status_string"]
 
 _lib = None
 

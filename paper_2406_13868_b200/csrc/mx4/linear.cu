@@ -516,6 +516,7 @@ static cudaError_t with_smem(K kern, uint32_t bytes, DeviceInfo* d, int bit) {
   return e;
 }
 constexpr uint32_t SMEM_MAX = 232448, NARROW_LEAST = 112640;
+static_assert(NARROW_LEAST == shared_for_columns(0, 256) && SMEM_MAX >= shared_for_columns(0, 512));
 
 // CTAs that share K of a row tile in the narrow kernel: as many as keep all of them resident, two an SM, with a tenth left over for clusters
 // that do not fit a GPU processing cluster (96 tiles x 3 of K = 4096 took 16.2 us, x 2 11.1); the sum over them is the dearer the more tokens there are
@@ -570,10 +571,7 @@ static sdq_status_t linear(GemmParams& p, DeviceInfo* d, void* stream) {
     if (parts > ring) p.nslot = (int32_t)((parts + slot - 1) / slot);
     lc.gridDim = dim3((unsigned)(p.n_tiles * ks), (unsigned)p.m_tiles);
     lc.blockDim = dim3(NARROW_THREADS);
-    // At least nearly half of an SM's (what two leave is for the next launch's small kernel): columns of tensor memory then always suffice for all
-    // that an SM has room for (256 here; the library's other products take 512 with more than half of the shared memory, 256 with half, or 128
-    // and run two an SM).  Beyond that, CTAs of two clusters could each hold the columns that the other's peer waits for, and a kernel in front
-    // that lets this one in before it has its own would wait for this one, which waits for it
+    // (nearly half of an SM's at least, for the 256 columns: see shared_for_columns)
     const uint32_t bytes = (uint32_t)p.nslot * slot + NARROW_TAIL;
     lc.dynamicSmemBytes = bytes > NARROW_LEAST ? bytes : NARROW_LEAST;
     attr[1].val.clusterDim.x = (unsigned)ks;

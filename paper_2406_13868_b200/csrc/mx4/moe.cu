@@ -671,7 +671,7 @@ static sdq_status_t moe(MoeParams p, DeviceInfo* d, void* stream) {
   p.unit = unit_pairs(p.T, pairs, p.E);
   p.max_units = (pairs < p.E ? pairs : p.E) + pairs / p.unit;
   // Few pairs an expert: both products in half an SM's shared and tensor memory, so that two CTAs of the first run on an SM, or the second's CTAs beside the
-  // first's, with their weights under way when h comes.  More than 76 KB each in any case: never a third such CTA on an SM, which tensor memory would not serve
+  // first's, with their weights under way when h comes (shared_for_columns: tensor memory serves whatever an SM has room for)
   const bool half = p.unit <= 16, few = p.T <= 16;
   p.tmem_cols = half ? 256 : 512;
   const uint32_t room = (half ? SMEM_MAX / 2 - 1024 : SMEM_MAX) - 1024 - 128;
@@ -698,7 +698,7 @@ static sdq_status_t moe(MoeParams p, DeviceInfo* d, void* stream) {
     const uint32_t behind = (uint32_t)p.unit * 1024u + (uint32_t)p.max_units * (uint32_t)sizeof(MoeUnit);
     p.ring_bytes = (int32_t)((room - behind) / 128 * 128);
     const int64_t cl = at_once / best < tasks ? at_once / best : tasks;
-    Launch l((unsigned)(cl * best), MOE_THREADS, (unsigned)best, (size_t)p.ring_bytes + behind + 128, stream);
+    Launch l((unsigned)(cl * best), MOE_THREADS, (unsigned)best, shared_for_columns((size_t)p.ring_bytes + behind + 128, p.tmem_cols), stream);
     const sdq_status_t st = launch_status(cudaLaunchKernelEx(&l.lc, up, p));
     if (st != SDQ_OK) return st;
   }
@@ -710,7 +710,7 @@ static sdq_status_t moe(MoeParams p, DeviceInfo* d, void* stream) {
     while (ks < 8 && 2 * ks * p.tiles_h <= 2 * d->sm_count && 2 * ks <= p.max_units * p.off.si) ks *= 2;
     const uint32_t room = SMEM_MAX / 2 - 1024 - 1024 - 128, behind = (uint32_t)p.T * 512u + (uint32_t)pairs * 8u + (uint32_t)p.max_units * (uint32_t)sizeof(MoeUnit);
     p.ring_bytes = (int32_t)((room - behind) / 128 * 128);
-    Launch l((unsigned)(p.tiles_h * ks), MOE_THREADS, (unsigned)ks, (size_t)p.ring_bytes + behind + 128, stream);
+    Launch l((unsigned)(p.tiles_h * ks), MOE_THREADS, (unsigned)ks, shared_for_columns((size_t)p.ring_bytes + behind + 128, p.tmem_cols), stream);
     return launch_status(cudaLaunchKernelEx(&l.lc, down, p));
   }
 }

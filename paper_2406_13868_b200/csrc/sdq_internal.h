@@ -36,6 +36,18 @@ DeviceInfo* device_info_slot(int dev);
 // entry of the current device with sm_count filled in (nullptr on failure).  First use per device takes a lock.
 DeviceInfo* device_info();
 
+// Dynamic shared memory of a thread block that takes `columns` columns of tensor memory and needs `bytes`: at least so much that its columns are
+// there whenever an SM has room for it.  An SM is given thread blocks by their threads, registers and shared memory (228 KB, 1 KB of it
+// reserved for each); of its 512 columns of tensor memory whoever places them knows nothing, and a thread block whose columns are taken waits
+// for them, without a limit, while its cluster's others may wait for it.  Two clusters, of one launch, of two streams or of a launch that was let in early, could
+// so hold the columns that each other's peers wait for.  With a quarter of the shared memory for 128 columns, nearly half for 256 and
+// what leaves less than a quarter for 512, no set of thread blocks that an SM has room for asks for more than 512.
+constexpr int SM_SHARED = 233472, SHARED_RESERVED = 1024;
+constexpr size_t shared_for_columns(size_t bytes, int columns) {
+  const size_t least = columns <= 128 ? SM_SHARED / 4 - SHARED_RESERVED : columns <= 256 ? 112640 : 3 * (SM_SHARED / 4);
+  return bytes > least ? bytes : least;
+}
+
 // status of a launch that returned `e`; takes the thread's last error with it, or the next call would report it as its own
 inline sdq_status_t launch_status(cudaError_t e) {
   const cudaError_t last = cudaGetLastError();

@@ -575,6 +575,47 @@ static LinearRoute linear_route(int64_t M, int64_t N, int64_t K, const sdq_confi
   return r;
 }
 
+// Geometry of a launch of this file's kernel (p.M, N, K and the format are there); returns the thread blocks to launch
+static int few_geometry(LinearParams& p, const LinearRoute& route, int sm_count) {
+  p.n_tile = n_tile_for(p.M);
+  p.slot_bytes = slot_bytes_for(p.n_tile, p.b32 != 0, p.dense != 0);
+  p.ksplit = route.ksplit;
+  p.cluster_ks = route.cluster_ks;
+  p.total_tiles = (int)(p.N / TILE_ROWS) * p.ksplit;
+  // ring geometry: a CTA that runs a single tile with no more stages than fit never reuses a slot, needs only as
+  // much shared memory as its stages, or its columns of tensor memory, take (so that small CTAs share an SM) and skips the slot-release traffic
+  const int T1 = p.out_n ? (int)(p.K / K1) : 0, T2 = (int)(p.K / K2);
+  const int stages_per_tile = (T2 + p.ksplit - 1) / p.ksplit + (T1 + p.ksplit - 1) / p.ksplit;
+  int max_slots = RING_BYTES / p.slot_bytes;
+  if (p.cluster_ks > 1 && p.total_tiles > sm_count) {
+    // cluster split K with more CTAs than SMs (few tokens, one tile per CTA): the grid is one wave only if two CTAs
+    // share an SM, so a ring gets half of an SM's shared memory (228 KB, 1 KB of it reserved per CTA)
+    const int half = (233472 / 2 - 1024 - SM_TAIL) / p.slot_bytes;
+    if (half < max_slots) max_slots = half;
+  }
+  if (max_slots > MAX_SLOTS) max_slots = MAX_SLOTS;
+  int grid_x;
+  if (p.total_tiles <= 2 * sm_count && stages_per_tile <= max_slots && p.n_tile <= 32) {
+    grid_x = p.total_tiles;
+    p.nslot = stages_per_tile;
+    p.release = 0;
+  } else if (p.cluster_ks > 1) {
+    grid_x = p.total_tiles;          // one tile per CTA (the cluster reduction relies on it); total_tiles <= SM count
+    p.nslot = max_slots;
+    p.release = 1;
+  } else {
+    grid_x = p.total_tiles < sm_count ? p.total_tiles : sm_count;
+    p.nslot = max_slots;
+    p.release = 1;
+  }
+  p.ring_bytes = p.nslot * p.slot_bytes;
+  p.meta_col = p.n_tile < 32 ? 32 : p.n_tile;
+  int cols = p.meta_col + (int)TM_META_COLS;
+  p.tmem_cols = cols <= 128 ? 128 : (cols <= 256 ? 256 : 512);
+  return grid_x;
+}
+static size_t few_shared(const LinearParams& p) { return shared_for_columns((size_t)p.ring_bytes + SM_TAIL, p.tmem_cols); }
+
 static sdq_status_t launch_linear(const sdq_act_t* Xq, const sdq_packed_t* P, void* Y, int64_t ldy, void* ws, size_t ws_bytes,
                                   void* stream, bool f32)
 {
@@ -624,11 +665,8 @@ static sdq_status_t launch_linear(const sdq_act_t* Xq, const sdq_packed_t* P, vo
     return launch_status(launch_linear_group(g, f32, dinfo, (cudaStream_t)stream));
   }
   if (route.kernel == SDQ_DIAG_PAIRS) return launch_status(launch_linear_pair(p, f32, dinfo, (cudaStream_t)stream));
-  p.n_tile = n_tile_for(M);
-  p.slot_bytes = slot_bytes_for(p.n_tile, p.b32 != 0, p.dense != 0);
   const int tiles = (int)(P->N / TILE_ROWS);
-  p.ksplit = route.ksplit;
-  p.cluster_ks = route.cluster_ks;
+  const int grid_x = few_geometry(p, route, sm_count);
   if (p.ksplit > 1 && p.cluster_ks == 1) {
     size_t need = 0;
     sdq_workspace_size(M, P->N, P->K, &P->cfg, &need);
@@ -636,42 +674,10 @@ static sdq_status_t launch_linear(const sdq_act_t* Xq, const sdq_packed_t* P, vo
     p.ws_counter = (uint32_t*)ws;
     p.ws_partial = (float*)((uint8_t*)ws + (((size_t)tiles * 4 + 255) & ~(size_t)255));
   }
-  p.total_tiles = tiles * p.ksplit;
-  // ring geometry: a CTA that runs a single tile with no more stages than fit never reuses a slot, needs only as
-  // much shared memory as its stages take (so that small CTAs share an SM) and skips the slot-release traffic
-  const int T1 = p.out_n ? (int)(P->K / K1) : 0, T2 = (int)(P->K / K2);
-  const int stages_per_tile = (T2 + p.ksplit - 1) / p.ksplit + (T1 + p.ksplit - 1) / p.ksplit;
-  int max_slots = RING_BYTES / p.slot_bytes;
-  if (p.cluster_ks > 1 && p.total_tiles > sm_count) {
-    // cluster split K with more CTAs than SMs (few tokens, one tile per CTA): the grid is one wave only if two CTAs
-    // share an SM, so a ring gets half of an SM's shared memory (228 KB, 1 KB of it reserved per CTA)
-    const int half = (233472 / 2 - 1024 - SM_TAIL) / p.slot_bytes;
-    if (half < max_slots) max_slots = half;
-  }
-  if (max_slots > MAX_SLOTS) max_slots = MAX_SLOTS;
-  int grid_x;
-  if (p.total_tiles <= 2 * sm_count && stages_per_tile <= max_slots && p.n_tile <= 32) {
-    grid_x = p.total_tiles;
-    p.nslot = stages_per_tile;
-    p.release = 0;
-  } else if (p.cluster_ks > 1) {
-    grid_x = p.total_tiles;          // one tile per CTA (the cluster reduction relies on it); total_tiles <= SM count
-    p.nslot = max_slots;
-    p.release = 1;
-  } else {
-    grid_x = p.total_tiles < sm_count ? p.total_tiles : sm_count;
-    p.nslot = max_slots;
-    p.release = 1;
-  }
-  p.ring_bytes = p.nslot * p.slot_bytes;
-  p.meta_col = p.n_tile < 32 ? 32 : p.n_tile;
-  int cols = p.meta_col + (int)TM_META_COLS;
-  p.tmem_cols = cols <= 128 ? 128 : (cols <= 256 ? 256 : 512);
-  const int smem = p.ring_bytes + SM_TAIL;
   cudaLaunchConfig_t lc = {};
   lc.gridDim = dim3((unsigned)grid_x);
   lc.blockDim = dim3(LIN_THREADS);
-  lc.dynamicSmemBytes = (size_t)smem;
+  lc.dynamicSmemBytes = few_shared(p);
   lc.stream = (cudaStream_t)stream;
   // the kernel may be scheduled while the previous one in the stream drains: set-up and weight copies overlap its tail
   cudaLaunchAttribute attr[2];
@@ -863,6 +869,34 @@ extern "C" sdq_status_t sdq_diag_linear_rings(int64_t M, int64_t N, int64_t K, c
   if (plan.kernel != SDQ_DIAG_PAIRS) return SDQ_OK;
   if (!diag_machine(sm_count, max_clusters)) return SDQ_ERR_CUDA;
   pair_describe_rings(pair_params(M, N, K, *cfg), sm_count, max_clusters, out);
+  return SDQ_OK;
+}
+
+extern "C" sdq_status_t sdq_diag_linear_memory(int64_t M, int64_t N, int64_t K, const sdq_config_t* cfg, int workspace, int sm_count, const int* max_clusters,
+                                               int32_t* shared, int32_t* columns)
+{
+  sdq_diag_plan_t plan;
+  if (!shared || !columns) return SDQ_ERR_INVALID_ARG;
+  const sdq_status_t st = sdq_diag_linear_plan(M, N, K, cfg, workspace, sm_count, max_clusters, &plan, nullptr, 0);
+  if (st != SDQ_OK) return st;
+  if (!diag_machine(sm_count, max_clusters)) return SDQ_ERR_CUDA;
+  LinearParams p = pair_params(M, N, K, *cfg);
+  if (plan.kernel == SDQ_DIAG_FEW) {
+    (void)few_geometry(p, linear_route(M, N, K, *cfg, workspace != 0, sm_count, max_clusters), sm_count);
+    *shared = (int32_t)few_shared(p); *columns = p.tmem_cols;
+  } else {
+    *shared = plan.kernel == SDQ_DIAG_PAIRS ? pair_describe_shared(p, sm_count, max_clusters) : group_shared(plan.token_tile, cfg->out_n, 0);
+    *columns = 512;
+  }
+  return SDQ_OK;
+}
+
+extern "C" sdq_status_t sdq_diag_group_memory(int64_t M, int64_t K, int out_n, int activations, int32_t* shared, int32_t* columns)
+{
+  if (!shared || !columns || out_n < 0 || out_n > 1) return SDQ_ERR_INVALID_ARG;
+  if (M <= 0 || M > 32 || K < 4 * K2 || K % K2 || (activations && (M > 16 || K > 16 * K2 || !group_xres_fits((int)(K / K2), out_n)))) return SDQ_ERR_SHAPE;
+  *shared = group_shared(M <= 16 ? 16 : 32, out_n, activations ? (int)(K / K2) : 0);
+  *columns = 512;
   return SDQ_OK;
 }
 

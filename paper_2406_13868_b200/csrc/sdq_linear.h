@@ -76,6 +76,7 @@ struct GroupParams {
 };
 cudaError_t launch_linear_group(GroupParams p, bool f32_out, DeviceInfo* d, cudaStream_t stream);
 double group_kernel_us(int64_t items, int T2, int sm_count, const int* max_clusters);   // estimated time of a call of `items` row tiles of 256 T2 K, in us
+int group_shared(int n_tile, int out_n, int x_T2);   // dynamic shared memory of a thread block (x_T2: K / 256 of the activation-resident variant, else 0)
 bool group_xres_fits(int T2, int out_n);   // the activation-resident variant's shared-memory budget for K = 256 T2
 
 // CTA-pair (tcgen05 cta_group::2) many-token kernel (sdq_linear_pair.cu).
@@ -85,6 +86,7 @@ double pair_kernel_us(int64_t M, int64_t N, int64_t K, int out_n, bool b32, bool
 const int* pair_max_clusters(DeviceInfo* d);
 // what sdq_diag_linear_plan and sdq_diag_group_plan report (the parameters as for a launch, pointers unset)
 void pair_describe_rings(LinearParams p, int sm_count, const int* max_clusters, sdq_diag_rings_t* out);
+int pair_describe_shared(LinearParams p, int sm_count, const int* max_clusters);     // dynamic shared memory of a thread block
 void pair_describe(LinearParams p, int sm_count, const int* max_clusters, sdq_diag_plan_t* out, sdq_diag_task_t* tasks, int64_t cap);
 void group_describe(GroupParams p, int sm_count, const int* max_clusters, sdq_diag_plan_t* out, sdq_diag_task_t* segs, int64_t cap);
 cudaError_t launch_linear_pair(LinearParams p, bool f32_out, DeviceInfo* d, cudaStream_t stream);

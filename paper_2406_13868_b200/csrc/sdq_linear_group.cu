@@ -645,6 +645,13 @@ static int group_units(int n_tile, int out_n, int xres_bytes) {
   return n > GRP_MAX_IN ? GRP_MAX_IN : n;
 }
 
+int group_shared(int n_tile, int out_n, int x_T2) {
+  const int xres_bytes = x_T2 ? group_xres_bytes(x_T2) : 0;
+  const int is = xres_bytes ? WI_BYTES : group_is_bytes(n_tile), os = out_n ? 2 * wc_bytes(1) + (xres_bytes ? 0 : 2 * n_tile * 128) : 0;
+  return (int)shared_for_columns((size_t)(group_units(n_tile, out_n, xres_bytes) * is + GRP_UNITS * os + xres_bytes + (out_n ? GRP_SIDE_BYTES : 0) + GRP_BAR_BYTES + 128),
+                                 (int)GRP_TMEM_COLS);
+}
+
 // shared-memory budget of the activation-resident variant: do at least six inlier slots fit beside X of K / 256 = T2 units?
 bool group_xres_fits(int T2, int out_n) { return group_units(16, out_n, group_xres_bytes(T2)) >= 6; }
 
@@ -713,9 +720,8 @@ cudaError_t launch_linear_group(GroupParams p, bool f32_out, DeviceInfo* d, cuda
   const GroupPlan plan = group_deal(p, d->sm_count, pair_max_clusters(d));
   const bool xres = p.x_bf16 != nullptr;
   const int xbytes = xres ? group_xres_bytes(p.m[0].T2) : 0;
-  const int is = xres ? WI_BYTES : group_is_bytes(p.n_tile), os = p.out_n ? 2 * wc_bytes(1) + (xres ? 0 : 2 * p.n_tile * 128) : 0;
   p.nslot = group_units(p.n_tile, p.out_n, xbytes);
-  const int smem = p.nslot * is + GRP_UNITS * os + xbytes + (p.out_n ? GRP_SIDE_BYTES : 0) + GRP_BAR_BYTES + 128;
+  const int smem = group_shared(p.n_tile, p.out_n, xres ? p.m[0].T2 : 0);
   if (!d->group_attr) {
     const cudaFuncAttribute a = cudaFuncAttributeMaxDynamicSharedMemorySize;
     bool ok = true;

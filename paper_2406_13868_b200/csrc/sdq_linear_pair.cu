@@ -664,7 +664,7 @@ static cudaError_t launch_form(const LinearParams& p, int pairs, cudaStream_t st
   cudaLaunchConfig_t lc = {};
   lc.gridDim = dim3((unsigned)(2 * p.pt_ks * pairs));
   lc.blockDim = dim3(PAIR_THREADS);
-  lc.dynamicSmemBytes = (size_t)p.ring_bytes + PAIR_TAIL;
+  lc.dynamicSmemBytes = shared_for_columns((size_t)p.ring_bytes + PAIR_TAIL, 512);
   lc.stream = stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -850,6 +850,12 @@ void pair_describe_rings(LinearParams p, int sm_count, const int* max_clusters, 
   out->slots = p.nslot; out->slot_bytes = p.slot_bytes;
   out->out_slots = p.pt_dual ? pair_slots(o) : p.nslot; out->out_slot_bytes = p.pt_dual ? (int)o : p.slot_bytes;
   out->bytes = p.ring_bytes;
+}
+
+int pair_describe_shared(LinearParams p, int sm_count, const int* max_clusters)
+{
+  (void)pair_apply(p, pair_best(p.M, p.N, p.K, p.out_n, p.b32 != 0, p.dense != 0, sm_count, max_clusters), sm_count);
+  return (int)shared_for_columns((size_t)p.ring_bytes + PAIR_TAIL, 512);
 }
 
 cudaError_t launch_linear_pair(LinearParams p, bool f32_out, DeviceInfo* d, cudaStream_t stream)
