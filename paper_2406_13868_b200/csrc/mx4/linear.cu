@@ -237,14 +237,15 @@ mx4_linear_narrow_kernel(const __grid_constant__ GemmParams p)
 }
 
 // ---- many tokens ----------------------------------------------------------------------------------------------------------
-constexpr int WIDE_THREADS = 512;                    // producer, MMA issuer, two idle, eight epilogue, four scale warps
+constexpr int WIDE_THREADS = 512;                    // producer, MMA issuer, one that tells of landed slots, an idle one, eight epilogue, four scale warps
 constexpr int WIDE_PAIRS = 4, WIDE_SETS = 4;
 // slots of the ring: what shared memory has beside the staging of outputs that are not aligned
 __host__ __device__ constexpr int wide_slots(int fmt, bool vec) { return fmt == SDQ_FMT_MXFP4 && vec ? 6 : 5; }
 // slot = | token record (codes, scale atoms) | codes of 128 weight rows | scale atoms of both CTAs' weight rows |
 __host__ __device__ constexpr uint32_t wide_slot(int fmt) { return record(fmt) + CODES + 2 * atoms(fmt) * ATOM; }
 // an arrival on a barrier of the pair's even CTA.  Relaxed: what it tells of, loads from and stores to tensor memory, has completed and been waited
-// for; a releasing arrival would wait for all of the thread's memory operations, a microsecond with a ring's copies under way
+// for, and is ordered by tcgen05's own fences; a releasing arrival would wait for all of the thread's memory operations, a microsecond with a ring's
+// copies under way.  It passes nothing on of shared memory: that a slot has landed, warp 2 tells
 __device__ __forceinline__ void arrive_leader(uint64_t* bar) {
   asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(ptx::mapa_u32(ptx::smem_u32(bar), 0)) : "memory");
 }
@@ -258,7 +259,7 @@ mx4_linear_wide_kernel(const __grid_constant__ GemmParams p)
   using T_out = typename Out<DT>::type;
   constexpr int WIDE_SLOTS = wide_slots(FMT, VEC);
   constexpr uint32_t NA = atoms(FMT), REC = record(FMT), SLOT = wide_slot(FMT), SFA_SET = 4u * NA, SET = 12u * NA;
-  static_assert(256 + WIDE_SETS * SET <= 512 && (6 + WIDE_PAIRS + 2 + WIDE_SETS) * 8 + 8 <= 256);
+  static_assert(256 + WIDE_SETS * SET <= 512 && (6 + WIDE_PAIRS + 2 + WIDE_SETS) * 8 + 8 + WIDE_SETS * 4 <= 256);
   constexpr uint32_t SL_B = REC, SL_SF = REC + CODES;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* sm = smem_raw + ((128 - (ptx::smem_u32(smem_raw) & 127)) & 127);
@@ -267,9 +268,10 @@ mx4_linear_wide_kernel(const __grid_constant__ GemmParams p)
   uint64_t* empty = full + WIDE_SLOTS;               // [pair of stages % WIDE_PAIRS]: the MMAs that read them have completed
   uint64_t* acc_full = empty + WIDE_PAIRS;
   uint64_t* acc_empty = acc_full + 1;
-  uint64_t* scales = acc_empty + 1;                  // [set] leader: slot landed and scales in tensor memory, in both CTAs
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(scales + WIDE_SETS);
+  uint64_t* ready = acc_empty + 1;                   // [set] leader: slot landed and scales in tensor memory, in both CTAs
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ready + WIDE_SETS);
   volatile uint32_t* timed_out = tmem_slot + 1;
+  uint32_t* told = tmem_slot + 2;                    // [set] leader: where the odd CTA's word that its slot has landed goes
   float* s_fac = reinterpret_cast<float*>(sm + WIDE_SLOTS * SLOT + 256);       // [task parity][factor, bias][256 weight rows]
   uint8_t* s_out = reinterpret_cast<uint8_t*>(s_fac + 4 * 256);
   const uint32_t rank = ptx::cluster_ctarank();
@@ -279,7 +281,7 @@ mx4_linear_wide_kernel(const __grid_constant__ GemmParams p)
 
   if (warp == 0 && lane == 0) {
     for (int i = 0; i < WIDE_SLOTS; ++i) ptx::mbar_init(&full[i], 1);
-    for (int i = 0; i < WIDE_SETS; ++i) ptx::mbar_init(&scales[i], 8);
+    for (int i = 0; i < WIDE_SETS; ++i) ptx::mbar_init(&ready[i], 9);
     for (int i = 0; i < WIDE_PAIRS; ++i) ptx::mbar_init(&empty[i], 1);
     ptx::mbar_init(acc_full, 1);
     ptx::mbar_init(acc_empty, 16);
@@ -342,7 +344,7 @@ mx4_linear_wide_kernel(const __grid_constant__ GemmParams p)
       int i = 0;
       for (int t = 0; t < my_tasks && ok; ++t) {
         for (int k = 0; k < KB; ++k, ++i) {
-          if (!(ok = ptx::mbar_wait_cluster(&scales[i % WIDE_SETS], ((uint32_t)i / WIDE_SETS) & 1u))) break;
+          if (!(ok = ptx::mbar_wait_cluster(&ready[i % WIDE_SETS], ((uint32_t)i / WIDE_SETS) & 1u))) break;
           if (k == 0 && t > 0 && !(ok = ptx::mbar_wait_cluster(acc_empty, (uint32_t)(t - 1) & 1u))) break;
           ptx::tc_fence_after();
           const uint32_t sfa = sets + (uint32_t)(i % WIDE_SETS) * SET, sfb = sfa + SFA_SET;
@@ -358,6 +360,30 @@ mx4_linear_wide_kernel(const __grid_constant__ GemmParams p)
           off += SLOT >> 4;
           if (off == (uint64_t)(SLOT >> 4) * WIDE_SLOTS) off = 0;
         }
+      }
+      if (!ok) atomicOr(&p.flags[FLAG_TIMEOUT], 1u);
+    }
+    __syncwarp();
+  } else if (warp == 2) {
+    // Tells the thread that issues the MMAs that a slot has landed.  In the leader by an arrival, in the odd CTA by an asynchronous store of a word that
+    // this arrival expects: its completion on the leader's barrier is a release at cluster scope, for which nobody waits here.  (A releasing arrival
+    // there takes a microsecond under load, 8192 x 4096 -> 11008 265 us against 171, or 195 with two warps in turn; barriers of their own that the
+    // issuing thread waits for as well, 190.)  Like the scale warps, not before the barrier's phase in front has completed
+    if (lane == 0) {
+      const uint32_t bar = ptx::mapa_u32(ptx::smem_u32(ready), 0), at = ptx::mapa_u32(ptx::smem_u32(told), 0);
+      const int total = my_tasks * KB;
+      uint32_t s = 0, ph = 0;
+      for (int i = 0; i < total; ++i) {
+        ok = ptx::mbar_wait(&full[s], ph);
+        if (ok && i >= WIDE_SETS) {
+          const uint32_t e = (uint32_t)(i - WIDE_SETS) >> 1;
+          ok = ptx::mbar_wait(&empty[e % WIDE_PAIRS], (e / WIDE_PAIRS) & 1u);
+        }
+        if (!ok) break;
+        const uint32_t set = (uint32_t)i % WIDE_SETS;
+        if (rank == 0) ptx::mbar_expect_tx(&ready[set], 4);
+        else ptx::st_async_u32(at + 4 * set, 0u, bar + 8 * set);
+        if (++s == WIDE_SLOTS) { s = 0; ph ^= 1u; }
       }
       if (!ok) atomicOr(&p.flags[FLAG_TIMEOUT], 1u);
     }
@@ -395,7 +421,7 @@ mx4_linear_wide_kernel(const __grid_constant__ GemmParams p)
       ptx::tmem_st_wait();
       ptx::tc_fence_before();
       __syncwarp();
-      if (lane == 0) arrive_leader(&scales[i % WIDE_SETS]);
+      if (lane == 0) arrive_leader(&ready[i % WIDE_SETS]);
       if (++s == WIDE_SLOTS) s = 0;
     }
     if (!ok && lane == 0) atomicOr(&p.flags[FLAG_TIMEOUT], 1u);

@@ -1,0 +1,46 @@
+"""Orders of the microscaled 4-bit kernels, read from the sources by what each role of a kernel does."""
+import re
+
+import pytest
+
+from tests.test_mx4_sources import kernels
+
+
+@pytest.fixture()
+def bodies(monkeypatch):
+    return {n: b for _, n, b in kernels(monkeypatch)}
+
+
+def roles(body):
+    """the branches of the first chain over the warp's number: condition -> code, comments aside"""
+    at = body.index("if (warp == 0)", body.index("bool ok = true;"))
+    out = {}
+    while True:
+        cond = re.compile(r"(?:else )?if \((warp[^{]*)\) \{").match(body, at)
+        if not cond:
+            return out
+        depth, end = 1, cond.end()
+        while depth:
+            depth += {"{": 1, "}": -1}.get(body[end], 0)
+            end += 1
+        out[cond.group(1)] = body[cond.end():end]
+        at = end + (1 if body[end] == " " else 0)
+
+
+def test_the_odd_cta_s_operands_are_passed_on_with_release(bodies):
+    """the thread that issues a pair's MMAs learns that the other CTA's copies have landed from a thread that has waited for them, through an operation that releases at
+    cluster scope, and acquires at that scope; arrivals without release carry nothing of shared memory and come on top"""
+    parts = roles(bodies["mx4_linear_wide_kernel"])
+    issuer = parts["warp == 1"]
+    waits = re.findall(r"mbar_wait_cluster\(&(\w+)\[", issuer)
+    assert len(waits) == 1 and issuer.index("mbar_wait_cluster") < issuer.index("ptx::mma2_")          # (acquire at cluster scope, for every stage)
+    bar = waits[0]
+    tells = [r for r in parts.values() if "st_async" in r or re.search(r"arrive\.release\.cluster", r)]
+    assert len(tells) == 1
+    tell = tells[0]
+    assert "ptx::mapa_u32(ptx::smem_u32(%s), 0)" % bar in tell and "mbar_expect_tx(&%s[" % bar in tell     # (that very barrier, in the leader)
+    assert tell.index("mbar_wait(&full[") < tell.index("mbar_wait(&empty[") < tell.index("mbar_expect_tx") and tell.index("mbar_wait(&empty[") < tell.rindex("st_async")
+    # whoever arrives there is counted: the scales' four warps of both CTAs, and the leader's expectation of the odd CTA's word
+    scales = [r for r in parts.values() if "arrive_leader(&%s[" % bar in r]
+    assert len(scales) == 1 and "mbar_init(&%s[i], 9)" % bar in bodies["mx4_linear_wide_kernel"]
+    assert scales[0].index("tmem_st_wait") < scales[0].index("tc_fence_before") < scales[0].index("arrive_leader")
