@@ -503,7 +503,7 @@ nv4_quantize_stream_kernel(const typename Elem<DT>::type* __restrict__ X, Shape 
   int n = 0, turn = 0;
   uint32_t ph = 0;
   for (int64_t b = blockIdx.x; b < blocks; b += gridDim.x, turn ^= 1) {
-    if (!wait32(ptx::smem_u32(&full[n]), ph)) { if (lane == 0) atomicOr(&flags[FLAG_TIMEOUT], 1u); return; }
+    const bool landed = __all_sync(0xffffffffu, wait32(ptx::smem_u32(&full[n]), ph));
     const uint8_t* row = ring + ((uint32_t)n * RB + rl) * row_bytes;
     const int64_t r = b * RB + rl;
     const bool have = r < s.R;
@@ -544,7 +544,16 @@ nv4_quantize_stream_kernel(const typename Elem<DT>::type* __restrict__ X, Shape 
 #pragma unroll
     for (int o = 1; o < LPR; o <<= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
     if (lane % LPR == 0) s_max[turn][warp][rl] = a;
-    __syncthreads();
+    if (!__syncthreads_and(landed)) {                        // a wait gave up: all warps leave, behind the copies that are still under way
+      if (tid == 0) {
+        atomicOr(&flags[FLAG_TIMEOUT], 1u);
+        for (int i = 0; i < buffers && b + (int64_t)i * gridDim.x < blocks; ++i) {
+          (void)wait32(ptx::smem_u32(&full[n]), ph);
+          if (++n == buffers) { n = 0; ph ^= 1u; }
+        }
+      }
+      return;
+    }
 #pragma unroll
     for (int w = 0; w < NS_WARPS; ++w) a = fmaxf(a, s_max[turn][w][rl]);
     const int t = nv_row_exp(fminf(a, type_max<DT>()));

@@ -44,3 +44,21 @@ def test_the_odd_cta_s_operands_are_passed_on_with_release(bodies):
     scales = [r for r in parts.values() if "arrive_leader(&%s[" % bar in r]
     assert len(scales) == 1 and "mbar_init(&%s[i], 9)" % bar in bodies["mx4_linear_wide_kernel"]
     assert scales[0].index("tmem_st_wait") < scales[0].index("tc_fence_before") < scales[0].index("arrive_leader")
+
+
+def test_a_streaming_quantizer_whose_wait_gives_up_leaves_as_a_whole(bodies):
+    """whether a wait gave up is decided for the thread block, at a barrier that all warps reach; its flag is set whichever lane saw it, and
+    the copies under way into its shared memory are waited for"""
+    b = bodies["nv4_quantize_stream_kernel"]
+    wait = re.search(r"const bool (\w+) = __all_sync\(0xffffffffu, wait32\(ptx::smem_u32\(&full\[n\]\), ph\)\);", b)
+    assert wait
+    left = b[b.index("if (!__syncthreads_and(%s))" % wait.group(1)):]
+    depth, end = 0, left.index("{")
+    while True:
+        depth += {"{": 1, "}": -1}.get(left[end], 0)
+        end += 1
+        if not depth:
+            break
+    gone = left[:end]
+    assert gone.index("atomicOr(&flags[FLAG_TIMEOUT], 1u)") < gone.index("wait32(") < gone.index("return;")
+    assert len(re.findall(r"\breturn;", b)) == 1 and b.count("wait32(") == 2          # (no other way out)
