@@ -167,7 +167,7 @@ mx4_linear_narrow_kernel(const __grid_constant__ GemmParams p)
         if (at.s == 0) off = 0;
       }
       if (ok) ptx::tc_commit(acc_full);
-      else atomicOr(&p.flags[FLAG_TIMEOUT], 1u);
+      else { atomicOr(&p.flags[FLAG_TIMEOUT], 1u); wait_for_copies(at, NSLOT); }
     }
     __syncwarp();
   } else if (warp >= 4) {
@@ -372,9 +372,9 @@ mx4_linear_wide_kernel(const __grid_constant__ GemmParams p)
     if (lane == 0) {
       const uint32_t bar = ptx::mapa_u32(ptx::smem_u32(ready), 0), at = ptx::mapa_u32(ptx::smem_u32(told), 0);
       const int total = my_tasks * KB;
-      uint32_t s = 0, ph = 0;
+      Slot at_slot(full, full, sm, 0);
       for (int i = 0; i < total; ++i) {
-        ok = ptx::mbar_wait(&full[s], ph);
+        ok = wait32(at_slot.full, at_slot.ph);
         if (ok && i >= WIDE_SETS) {
           const uint32_t e = (uint32_t)(i - WIDE_SETS) >> 1;
           ok = ptx::mbar_wait(&empty[e % WIDE_PAIRS], (e / WIDE_PAIRS) & 1u);
@@ -383,9 +383,9 @@ mx4_linear_wide_kernel(const __grid_constant__ GemmParams p)
         const uint32_t set = (uint32_t)i % WIDE_SETS;
         if (rank == 0) ptx::mbar_expect_tx(&ready[set], 4);
         else ptx::st_async_u32(at + 4 * set, 0u, bar + 8 * set);
-        if (++s == WIDE_SLOTS) { s = 0; ph ^= 1u; }
+        at_slot.next(WIDE_SLOTS, SLOT);
       }
-      if (!ok) atomicOr(&p.flags[FLAG_TIMEOUT], 1u);
+      if (!ok) { atomicOr(&p.flags[FLAG_TIMEOUT], 1u); wait_for_copies(at_slot, WIDE_SLOTS); }
     }
     __syncwarp();
   } else if (warp >= 12) {
@@ -524,6 +524,7 @@ mx4_linear_wide_kernel(const __grid_constant__ GemmParams p)
         }
       }
     }
+    if (!ok && lane == 0) atomicOr(&p.flags[FLAG_TIMEOUT], 1u);
     __syncwarp();
   }
   // (a peer may still signal barriers of this CTA, and its MMAs read this CTA's shared memory)

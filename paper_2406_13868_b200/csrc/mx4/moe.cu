@@ -395,7 +395,7 @@ moe_up_kernel(const __grid_constant__ MoeParams p)
         }
         if (ok) ptx::tc_commit(&b.acc_full[buf]);
       }
-      if (!ok) atomicOr(&p.flags[FLAG_TIMEOUT], 1u);
+      if (!ok) { atomicOr(&p.flags[FLAG_TIMEOUT], 1u); wait_for_copies(at, NSLOT); }
     }
     __syncwarp();
   } else if (warp >= 4) {
@@ -577,7 +577,7 @@ moe_down_kernel(const __grid_constant__ MoeParams p)
         }
         if (ok) ptx::tc_commit(&b.acc_full[buf]);
       }
-      if (!ok) atomicOr(&p.flags[FLAG_TIMEOUT], 1u);
+      if (!ok) { atomicOr(&p.flags[FLAG_TIMEOUT], 1u); wait_for_copies(at, NSLOT); }
     }
     __syncwarp();
   } else if (warp >= 4 && warp < 8) {

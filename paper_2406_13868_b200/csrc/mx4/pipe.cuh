@@ -16,9 +16,9 @@ __device__ __forceinline__ bool test32(uint32_t bar, uint32_t parity) {
   asm volatile("{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok != 0;
 }
-__device__ __forceinline__ bool wait32(uint32_t bar, uint32_t parity) {
+__device__ __forceinline__ bool wait32(uint32_t bar, uint32_t parity, uint32_t limit = 1u << 22) {
   uint32_t ok = test32(bar, parity);
-  for (uint32_t i = 0; !ok && i < (1u << 22); ++i)
+  for (uint32_t i = 0; !ok && i < limit; ++i)
     asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok != 0;
 }
@@ -57,6 +57,16 @@ struct Slot {
     if (s == n) { s = 0; ph ^= 1u; full -= 8 * n; empty -= 8 * n; at -= size * n; }
   }
 };
+
+// for the thread that empties a ring, whose wait gave up at `at`: waits, with a limit, for the copies that may still be under way, those of a lap from there
+// on, so that none is left when the shared memory becomes another thread block's (who calls this is waited for before the thread block can leave)
+__device__ __forceinline__ void wait_for_copies(Slot at, uint32_t slots) {
+#pragma unroll 1
+  for (uint32_t i = 0; i < slots; ++i) {
+    (void)wait32(at.full, at.ph, 1u << 16);
+    at.next(slots, 0);
+  }
+}
 
 }  // namespace mx4
 }  // namespace sdq

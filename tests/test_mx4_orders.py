@@ -13,7 +13,7 @@ def bodies(monkeypatch):
 
 def roles(body):
     """the branches of the first chain over the warp's number: condition -> code, comments aside"""
-    at = body.index("if (warp == 0)", body.index("bool ok = true;"))
+    at = re.compile(r"if \(warp == 0[^{]*\) \{").search(body, body.index("bool ok = true;")).start()
     out = {}
     while True:
         cond = re.compile(r"(?:else )?if \((warp[^{]*)\) \{").match(body, at)
@@ -39,7 +39,7 @@ def test_the_odd_cta_s_operands_are_passed_on_with_release(bodies):
     assert len(tells) == 1
     tell = tells[0]
     assert "ptx::mapa_u32(ptx::smem_u32(%s), 0)" % bar in tell and "mbar_expect_tx(&%s[" % bar in tell     # (that very barrier, in the leader)
-    assert tell.index("mbar_wait(&full[") < tell.index("mbar_wait(&empty[") < tell.index("mbar_expect_tx") and tell.index("mbar_wait(&empty[") < tell.rindex("st_async")
+    assert tell.index("wait32(at_slot.full, at_slot.ph)") < tell.index("mbar_wait(&empty[") < tell.index("mbar_expect_tx") and tell.index("mbar_wait(&empty[") < tell.rindex("st_async")
     # whoever arrives there is counted: the scales' four warps of both CTAs, and the leader's expectation of the odd CTA's word
     scales = [r for r in parts.values() if "arrive_leader(&%s[" % bar in r]
     assert len(scales) == 1 and "mbar_init(&%s[i], 9)" % bar in bodies["mx4_linear_wide_kernel"]
@@ -62,3 +62,25 @@ def test_a_streaming_quantizer_whose_wait_gives_up_leaves_as_a_whole(bodies):
     gone = left[:end]
     assert gone.index("atomicOr(&flags[FLAG_TIMEOUT], 1u)") < gone.index("wait32(") < gone.index("return;")
     assert len(re.findall(r"\breturn;", b)) == 1 and b.count("wait32(") == 2          # (no other way out)
+
+
+@pytest.mark.parametrize("kernel,role,by", [("mx4_linear_narrow_kernel", "warp == 1", "at"), ("mx4_linear_wide_kernel", "warp == 2", "at_slot"), ("moe_up_kernel", "warp == 1", "at"),
+                                            ("moe_down_kernel", "warp == 1", "at")])
+def test_a_thread_block_whose_wait_gives_up_waits_for_its_copies(bodies, kernel, role, by):
+    """the thread that empties the ring, in order, waits with a limit for what may still be under way; the barriers at the kernel's end lie behind it"""
+    body = bodies[kernel]
+    part = roles(body)[role]
+    assert re.search(r"\{ atomicOr\(&p\.flags\[FLAG_TIMEOUT\], 1u\); wait_for_copies\(%s, (NSLOT|WIDE_SLOTS)\); \}" % by, part)
+    assert re.search(r"wait32\(%s\.full, %s\.ph\)" % (by, by), part)
+    tail = body[body.index(part) + len(part):]
+    assert re.search(r"cluster_sync\(\)|__syncthreads\(\)", tail)
+
+
+@pytest.mark.parametrize("kernel", ["mx4_linear_narrow_kernel", "mx4_linear_wide_kernel", "moe_up_kernel", "moe_down_kernel"])
+def test_every_role_that_waits_reports_a_wait_that_gave_up(bodies, kernel):
+    """each of them, the epilogues too: the wait that gave up may be the only one"""
+    for cond, part in roles(bodies[kernel]).items():
+        if re.search(r"mbar_wait|wait32", part):
+            assert "atomicOr(&p.flags[FLAG_TIMEOUT], 1u)" in part, cond
+        elif "produce(" in part:
+            assert "p.flags" in part, cond
