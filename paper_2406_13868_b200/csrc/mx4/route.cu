@@ -40,6 +40,13 @@ __device__ __forceinline__ long long rank_key(double x) {
   const long long b = __double_as_longlong(x + 0.0);
   return b ^ ((b >> 63) & 0x7FFFFFFFFFFFFFFFll);
 }
+// largest of n numbers, a NaN aside (by a warp)
+__device__ __noinline__ double largest(const double* v, int n, uint32_t lane) {
+  double top = -INFINITY;
+  for (int i = (int)lane; i < n; i += 32) top = fmax(top, v[i]);
+  for (int o = 16; o; o >>= 1) top = fmax(top, __shfl_xor_sync(0xffffffffu, top, o));
+  return top;
+}
 __device__ __forceinline__ double warp_sum(double v) {
 #pragma unroll
   for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -75,9 +82,11 @@ __device__ __forceinline__ void choose(const RouteParams& p, int64_t t, double* 
     for (int e = (int)lane; e < p.E; e += 32) top = fmaxf(top, (float)score[e]);
     const int b = __float_as_int(top + 0.0f), k = __reduce_max_sync(0xffffffffu, b ^ (b >> 31 & 0x7FFFFFFF));
     top = __int_as_float(k ^ (k >> 31 & 0x7FFFFFFF));
+    // (from 2^30 on fp32 is off by more than 32, and further on by more than exp takes)
+    const double top64 = fabsf(top) < 1073741824.0f ? (double)top : largest(score, p.E, lane);
     __syncthreads();                                  // (everybody has read the logits)
     double sum = 0.0;
-    for (int e = (int)tid; e < p.E; e += THREADS) { const double v = exp(score[e] - (double)top); sum += v; score[e] = v; }
+    for (int e = (int)tid; e < p.E; e += THREADS) { const double v = exp(score[e] - top64); sum += v; score[e] = v; }
     if (!p.renorm || p.bias) {
       sum = warp_sum(sum);
       if (lane == 0) red[warp] = sum;
