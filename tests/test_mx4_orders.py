@@ -1,9 +1,10 @@
 """Orders of the microscaled 4-bit kernels, read from the sources by what each role of a kernel does."""
+import os
 import re
 
 import pytest
 
-from tests.test_mx4_sources import kernels
+from tests.test_mx4_sources import MX4, kernels
 
 
 @pytest.fixture()
@@ -84,3 +85,52 @@ def test_every_role_that_waits_reports_a_wait_that_gave_up(bodies, kernel):
             assert "atomicOr(&p.flags[FLAG_TIMEOUT], 1u)" in part, cond
         elif "produce(" in part:
             assert "p.flags" in part, cond
+
+
+READS = {                              # what reads global memory through more than a plain subscript -> kernels that do so
+    r"\bload16<": {"mx4_quantize_kernel", "nv4_quantize_kernel"},
+    r"(?<!auto )\bload\(": {"nv4_quantize_stream_kernel"},
+    r"\bcopy32\(": {"mx4_linear_narrow_kernel"},
+    r"\bbulk_g2s\(": {"mx4_linear_wide_kernel"},
+    r"\bget_codes\(": {"mx4_export_kernel", "mx4_dequantize_kernel"},
+    r"\bcodes\[r \* kb": {"mx4_import_kernel", "mx4_export_kernel"},
+    r"\bload8<": {"moe_route_kernel"},
+    r"\bload8_raw<": {"moe_route_mma_kernel"},
+    r"reinterpret_cast<const T\*>\(p\.x\)": {"moe_split_kernel"},
+}
+
+
+@pytest.mark.parametrize("what", list(READS))
+def test_reads_of_global_memory_lie_behind_the_wait(bodies, what):
+    """every kernel that reads so does it behind its wait for the launch in front (the expert layer's two products, which read what is complete before, aside)"""
+    found = set()
+    for n, b in bodies.items():
+        if n in ("moe_up_kernel", "moe_down_kernel"):
+            continue
+        if n == "nv4_quantize_stream_kernel" and "copy32" in what:
+            # (inside the function that the row before looks for the calls of)
+            load = b.index("auto load = [&]")
+            assert all(load < x.start() < b.index("};", load) for x in re.finditer(what, b))
+            continue
+        at = [x.start() for x in re.finditer(what, b)]
+        if at:
+            found.add(n)
+            assert min(at) > b.index("ptx::griddep_wait()"), n
+    assert found == READS[what]
+
+
+def test_every_kernel_that_is_given_operands_is_among_them(bodies):
+    assert set().union(*READS.values()) | {"moe_up_kernel", "moe_down_kernel"} == set(bodies)
+
+
+def test_row_maxima_are_exchanged_between_two_cluster_barriers(bodies):
+    """peers' shared memory is written when all of them have started, and read when all of them have written"""
+    src = re.sub(r"//[^\n]*", "", open(os.path.join(MX4, "quant.cu")).read())
+    at = src.index("__device__ __forceinline__ float max_over_cluster(")
+    body = src[src.index("{", at):src.index("\n}\n", at)]
+    alone, rest = body.split("if (ctas == 1) {", 1)
+    assert "cluster" not in alone and "return a;" in rest[:rest.index("}")]
+    remote = [x.start() for x in re.finditer(r"st\.shared::cluster", rest)]
+    syncs = [x.start() for x in re.finditer(r"ptx::cluster_sync\(\)", rest)]
+    assert len(syncs) == 2 and remote and syncs[0] < min(remote) <= max(remote) < syncs[1] < rest.index("m.cta[c][")
+    assert [n for n, b in bodies.items() if "max_over_cluster(" in b] == ["nv4_quantize_kernel"]
