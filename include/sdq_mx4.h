@@ -76,7 +76,9 @@ sdq_status_t sdq_mx4_experts_import(const uint8_t* codes, const uint8_t* scales,
 /* Router: logits = X Wr^T over the H channels, X [T][ldx] and Wr [E][ldw] of `dtype`; score = softmax over the E experts or
  * sigmoid; every token's k experts are those of the largest score + bias (bias (device) [E] fp32 or NULL; of equal ones the lowest
  * index first), in descending order; weight = score of the chosen, divided by their sum where `renorm`, times `scale`.
- * Logits, scores and choices are formed in 64 bits from fp32 partial sums.  ids (device) [T][k] int32, weights (device) [T][k] fp32.
+ * Logits, scores and choices are formed in 64 bits from fp32 partial sums: a logit is within 32 * 2^-23 (16-bit operands, sums of 32 products) or
+ * 8 * 2^-24 (fp32, sums of 8) of the sum of its products' magnitudes, and the choice does not depend on the order of the channels where the gaps are wider than
+ * that.  ids (device) [T][k] int32, weights (device) [T][k] fp32.
  * 1 <= k <= E <= 1024, k <= 32. */
 sdq_status_t sdq_moe_route(const void* X, int32_t dtype, int64_t T, int64_t H, int64_t ldx, const void* Wr, int64_t E, int64_t ldw,
                            const float* bias, int32_t k, int32_t scoring, int32_t renorm, float scale,
@@ -85,7 +87,7 @@ sdq_status_t sdq_moe_route(const void* X, int32_t dtype, int64_t T, int64_t H, i
 /* Experts: Y[t] = sum_j weights[t][j] * W2[e](silu(W1[e] x_t) * W3[e] x_t), e = ids[t][j].  X [T][ldx], Y [T][ldy] bf16 or fp16;
  * w1, w3 [E, I, H], w2 [E, H, I] in the experts' layout.  The activations are not quantized: the tensor core multiplies the 4-bit weights by
  * six E2M1 pieces whose sum is x, exactly down to 2^-9 (fp16: 2^-6) of the largest magnitude of its 32 channels and to 2^-17 of that
- * below; the same for silu(.) * (.) in fp32.  A pair whose id lies outside [0, E) adds nothing.  1 <= T <= 64, 1 <= k <= 32.  A token that
+ * below, and never finer than 2^-128; the same for silu(.) * (.) in fp32.  A pair whose id lies outside [0, E) adds nothing.  1 <= T <= 64, 1 <= k <= 32.  A token that
  * holds an infinity or a NaN gives NaN.
  * ws (device): scratch of sdq_mx4_moe_workspace_size bytes, needs no initialisation; calls that can overlap on the GPU must not
  * share it. */

@@ -80,7 +80,7 @@ __device__ __forceinline__ uint32_t piece_off(uint32_t r, uint32_t k) { return (
 
 // ---- pieces -------------------------------------------------------------------------------------------------------------------
 // code c of the block's scale 2^(c - 127), its largest magnitude lying in [2, 4) times it; at least 15, so that the later pieces' scales
-// (c - 3, .., c - 15) are codes too
+// (c - 3, .., c - 15) are codes too (blocks whose largest magnitude is below 2^-111 keep what lies above 2^-128)
 __device__ __forceinline__ uint32_t piece_scale(uint32_t amax_bits) { return (uint32_t)min(max((int)(amax_bits >> 23) - 1, 15), 253); }
 __device__ __forceinline__ float piece_inverse(uint32_t c) { return __uint_as_float((254u - c) << 23); }
 // scale code of piece i; a block that holds something not finite: NaN

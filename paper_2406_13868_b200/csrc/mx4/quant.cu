@@ -3,7 +3,11 @@
 // All of them work in units of 8 rows x 128 K, one a warp, as two halves of 64 K: lane l has row l / 4, elements 16 (l % 4) .. + 15 of a half.  An
 // access of a lane is 32 bytes (of a 16-bit type) and four lanes have a line of 128; a store of codes writes whole core matrices.
 //
-// Bound by DRAM traffic: 2 to 4 bytes an element on one side, 0.53 or 0.56 on the other.
+// What has to move are 2 to 4 bytes an element on one side and 0.53 or 0.56 on the other.  Dequantizer of many aligned rows: at DRAM's rate (8192 x 11008 38 us,
+// its bytes 36).  MXFP4 quantizer: near it (8192 x 4096 18 us under the profiler, bytes 13; DRAM 47 % there).  NVFP4 quantizer of many rows: its encode loop, three
+// dependent operations an element for an exact quotient (8192 x 11008 66 us, bytes 36).  Rows off every boundary: the granules' branches and shifts (1000 x
+// 4109 7.4 and 4.4 us, bytes 1.6).  Importer and exporter move bytes one by one, once for a checkpoint's matrix: 11008 x 4096 28 and 55 us, 1.7 and
+// 0.9 TB/s.  A few rows: a launch
 #include <cuda_fp16.h>
 
 #include <type_traits>
@@ -470,8 +474,8 @@ nv4_quantize_kernel(const typename Elem<DT>::type* __restrict__ X, Shape s, uint
 // Many long rows of a 16-bit type: one CTA an SM goes through them RB at a time, the next ones on their way into shared memory (bulk copies)
 // while these are read there twice, for the maxima and to be encoded.  A row is read from DRAM once and nothing waits for anybody else.
 // us, this and the cluster form: 8192 x 11008 bf16 67 and 99 (rows read again from L2: 82), 4096 x 16384 53 and 71, 512 x 11008 7.8 and 9.8; but 300 x
-// 11008 6.1 and 4.7, and where a warp of the cluster form has one unit, 2048 x 4096 10.9 and 9.4, 8192 x 4096 29.0 and 28.5.  Issue slots 56 %
-// taken, DRAM 54 %: the two passes and the barriers between them are what is left.
+// 11008 6.1 and 4.7, and where a warp of the cluster form has one unit, 2048 x 4096 10.9 and 9.4, 8192 x 4096 29.0 and 28.5.  Copies and
+// maxima alone take 28 of the 66 us at 8192 x 11008, without the encoding 47, without the stores 58: what is left is the encode loop, with issue slots 56 % taken and DRAM 54 %.
 constexpr int NS_WARPS = 16, NS_MAX_BUFFERS = 8;
 template <int DT, int RB>
 __global__ void __launch_bounds__(32 * NS_WARPS)

@@ -1,10 +1,11 @@
 // Router of an expert layer: logits of every token over the experts, scores, the k best and their weights, in one launch.
 //
 // A cluster takes a group of tokens; its CTAs share the experts, and K where there are few of them.  Each token's logits are gathered in the
-// shared memory of one CTA, which scores and chooses.  Which expert is chosen must not hang on the order of a sum: products of 16-bit
-// operands are exact in fp32, 32 of them are summed there, by the tensor core (mma.sync: sixteen experts x eight tokens, a shape that
-// this size of problem fills, where a tcgen05 tile would be all padding), and everything behind that in 64 bits.  fp32 operands go through
-// ordinary multiplications, eight to a sum.
+// shared memory of one CTA, which scores and chooses.  Which expert is chosen should hang on the order of a sum as little as
+// can be: products of 16-bit operands are exact in fp32, 32 of them are summed there, by the tensor core (mma.sync: sixteen experts x eight
+// tokens, a shape that this size of problem fills, where a tcgen05 tile would be all padding), which may cut what it adds, and everything
+// behind that in 64 bits.  fp32 operands go through ordinary multiplications, eight to a sum.  So a logit is within 32 2^-23 (16-bit operands) or
+// 8 2^-24 (fp32) of the sum of its products' magnitudes, and only experts nearer to each other than that may change places.
 #include "../sdq_internal.h"
 #include "../sdq_ptx.cuh"
 #include "layout.h"
