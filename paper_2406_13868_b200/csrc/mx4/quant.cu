@@ -283,7 +283,7 @@ __device__ __forceinline__ uint2 encode_nv(float (&v)[16], const NvRow& row, uin
   float a = max16(v);
   saturate<DT>(v, a);
   scale = a != a ? 127u : nv_scale_code<DT>(a * row.down, a > 0.0f);
-  const float s = e4m3_value(scale) * row.up;
+  const float s = fminf(e4m3_value(scale), 448.0f) * row.up;          // (a NaN's block: codes as under the largest scale, so that zeros, padding among them, stay zeros)
   float r;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
   if (scale == 0u) r = 0.0f;

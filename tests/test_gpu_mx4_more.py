@@ -80,3 +80,19 @@ def test_mxfp4_scales_of_all_sizes(m, lo, hi, M, N, K, dtype):
     fits = scale * (1 + K * 2.0 ** -23) + tol < top             # (no partial sum leaves the range)
     assert (np.abs(y - want)[fits] <= tol[fits]).all()
     assert not np.isfinite(y[np.abs(want) - tol > 2 * top]).any()
+
+
+@pytest.mark.parametrize("nv", [False, True])
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("R,K", [(3, 77), (3, 1), (700, 8201), (5, 4109), (2, 16401)])
+def test_padding_is_zero_in_a_nan_s_block_too(m, nv, dtype, R, K):
+    """the last byte of an odd row holds one code, whatever its block's scale is"""
+    fmt = m.FMT_NVFP4 if nv else m.FMT_MXFP4
+    x = inputs(R, K, DT[dtype], K, spread=False)
+    x[0, K - 1], x[R - 1, K - 1] = float("nan"), float("nan")
+    q = m.sdq_mx4_quantize(x.cuda(), fmt)
+    e = m.mx4_export(q)
+    assert (e["scale"][0, -1] == (127 if nv else 255)).all() and not (e["code"][:, -1] >> 4).any()
+    # and so a matrix that is exported and imported is the same one
+    again = m.mx4_export(m.sdq_mx4_import(e["code"], e["scale"], fmt, K=K, factor=e.get("factor")))
+    assert torch.equal(again["code"], e["code"]) and torch.equal(again["scale"], e["scale"])
